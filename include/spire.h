@@ -352,6 +352,184 @@ spire_status spire_feedback_memory(const void *x, int32_t x_dtype, const float *
                                    hipStream_t stream);
 
 /*
+ * ---- around the attention: pages, projections, latent caches -----------------
+ *
+ * A serving loop's step, all on the device: spire_page_extend gives the new
+ * tokens of every request their pages and slots, spire_qkv_append (grouped
+ * heads) or spire_latent_append (latent cache) brings the layer's projections
+ * into the cache, spire_verify_attn or spire_latent_verify_attn reads it, and
+ * spire_page_release takes back the pages of what was not accepted.
+ *
+ * A slot is a token's place in a cache: page * page_size + row of the page
+ * (paged storage), or sequence * capacity + row (contiguous storage).  -1, or
+ * any value without storage, is a token that is not stored.
+ */
+
+/* Bytes of workspace spire_page_extend and spire_page_release need (0 on invalid sizes). */
+size_t spire_page_workspace_size(int32_t B);
+
+/*
+ * Pages and slots for the next tokens of B requests.  Sequence b holds
+ * lens[b] tokens in ceil(lens[b] / page_size) pages, the first entries of its
+ * row of block_table, and gets new_tokens[b] more (negative counts as 0).
+ *   cu[b] = sum of new_tokens before b: token t of sequence b has index cu[b] + t.
+ *   Admission goes in the order of b: a sequence whose tokens do not fit its
+ *   table row (max_blocks * page_size) is refused; of the others, b is admitted
+ *   while the pages needed up to and with b are at most n_free and cu[b + 1] is
+ *   at most max_tokens, so the first that does not fit and all after it are
+ *   refused.  A refused sequence keeps its length and table row.
+ *   The i-th page handed out (in order of b, then of columns) is
+ *   free_pages[n_free - 1 - i]; it is entered in block_table.
+ *   free_pages [pool] int32: the ids [0, n_free) are free; read only.
+ *   n_free     [1] int32, clamped to [0, pool].
+ *   slots      [max_tokens] int64 out: the slot of every token, -1 for tokens of
+ *              refused sequences, for a negative page id and behind the last
+ *              token, so a batch padded to max_tokens can be appended as it is.
+ *   positions  [max_tokens] int32 out: lens[b] + t, 0 where no sequence is admitted.
+ *   cu_tokens  [B + 1] int32 out: cu (values beyond 2^31 - 1 read 2^31 - 1).
+ *   lens_out   [B] int32 out: the lengths afterwards; n_free_out [1] int32 out.
+ *              Both may be the arrays lens / n_free themselves.
+ *   sizes      0 <= B <= 8192, page_size >= 1, max_blocks >= 1, pool >= 0,
+ *              0 <= max_tokens <= 2^30.
+ *   workspace  >= spire_page_workspace_size(B) bytes, 256-byte aligned.
+ * Arrays other than those two pairs must not overlap.
+ */
+spire_status spire_page_extend(int32_t *block_table, int32_t page_size, int32_t max_blocks,
+                               const int32_t *lens, const int32_t *new_tokens, int32_t B,
+                               const int32_t *free_pages, int32_t pool, const int32_t *n_free,
+                               int64_t *slots, int32_t *positions, int32_t max_tokens,
+                               int32_t *cu_tokens, int32_t *lens_out, int32_t *n_free_out,
+                               void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Takes back the pages behind keep[b] tokens: sequence b, lens[b] tokens long,
+ * is cut to min(lens[b], max(keep[b], 0)), and the ids of table columns
+ * ceil(kept / page_size) .. ceil(lens[b] / page_size) - 1 are pushed on
+ * free_pages from n_free on, in order of b, then of columns (pushes beyond
+ * `pool` are dropped).  The table row is left as it is: entries behind a
+ * sequence's pages mean nothing.  Aliasing as for spire_page_extend.
+ */
+spire_status spire_page_release(const int32_t *block_table, int32_t page_size, int32_t max_blocks,
+                                const int32_t *lens, const int32_t *keep, int32_t B,
+                                int32_t *free_pages, int32_t pool, const int32_t *n_free,
+                                int32_t *lens_out, int32_t *n_free_out, void *workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Position rotation with one or several axes (text; time, height and width of
+ * images and video).  Pair i < rot_dim / 2 of token t turns by the angle
+ *   positions[axis[i]][t] * inv_freq[i]      (formed in fp64)
+ * (x, y) -> (x cos - y sin, y cos + x sin); pair i is elements (i, i + rot_dim/2),
+ * or (2i, 2i + 1) when interleaved.  Elements from rot_dim on pass unchanged.
+ */
+typedef struct spire_rope {
+    const int32_t *positions;    /* device [axes, N] int32 */
+    const float *inv_freq;       /* device [rot_dim / 2] fp32 */
+    const int32_t *axis;         /* device [rot_dim / 2] int32, clamped to [0, axes); NULL: axis 0 */
+    int32_t axes;                /* 1..8 */
+    int32_t rot_dim;             /* even; 0: no rotation (the pointers are not read) */
+    int32_t interleaved;         /* 0 or 1 */
+    int32_t reserved;            /* must be 0 */
+} spire_rope;
+
+/*
+ * The projections of N tokens on their way into a grouped-query cache, in one
+ * pass: queries and keys are normed per head and rotated, queries go to q_out,
+ * keys and values to their tokens' slots.
+ *   q [N, Hq, D], k and v [N, Hkv, D], in_dtype SPIRE_F32 or SPIRE_BF16: heads
+ *     are D elements apart, tokens q_stride / k_stride / v_stride elements (the
+ *     parts of one fused projection have its width).
+ *   norm: y = x / sqrt(mean(x^2) + eps) * w over the D elements of a head;
+ *     q_weight, k_weight [D] fp32, NULL: no norm of that part.  eps >= 0.
+ *   rope: the rotation, after the norm; NULL: none.  rot_dim <= D.
+ *   q_out [N, Hq, D] contiguous, out_dtype SPIRE_F32 or SPIRE_BF16.
+ *   kv    destination view; paged, or contiguous with num_blocks = its sequences.
+ *     Written at slots[t] (the block table is not read); rounded as for
+ *     spire_kv_append.  A slot outside [0, num_blocks * rows per block) is
+ *     skipped; two tokens with one slot leave either's row.
+ *   sizes  0 <= N < 2^31, 1 <= Hq, 1 <= Hkv, Hq + 2 Hkv <= 4096, 1 <= D <= 1024.
+ * Arithmetic in fp32, one rounding per stored element.  Outputs must not
+ * overlap inputs.  No workspace.
+ */
+spire_status spire_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                              const void *v, int64_t v_stride, int32_t in_dtype,
+                              const float *q_weight, const float *k_weight, float eps,
+                              const spire_rope *rope, const spire_kv *kv, const int64_t *slots,
+                              int32_t N, int32_t Hq, int32_t Hkv, int32_t D, void *q_out,
+                              int32_t out_dtype, hipStream_t stream);
+
+/*
+ * A latent cache: one row per token, Dc elements of the latent that keys and
+ * values of every head share, then Dr elements of the rotated key part.
+ * Element (blk, t, d) lives at c + (blk * s_blk + t * s_tok + d) * sizeof(dtype);
+ * paged and contiguous addressing as for spire_kv.  fp8: the value of a byte is
+ * decode(byte) * scale[0] (finite, > 0, one scale for the cache).
+ */
+typedef struct spire_latent {
+    const void *c;               /* device */
+    const int32_t *block_table;  /* device [B, max_blocks] int32, paged only (else NULL) */
+    const float *scale;          /* device [1] fp32, fp8 only (else NULL) */
+    int64_t s_blk;               /* element strides */
+    int64_t s_tok;
+    int32_t dtype;               /* spire_dtype */
+    int32_t Dc;                  /* latent elements */
+    int32_t Dr;                  /* rotated elements */
+    int32_t page_size;           /* 0 = contiguous */
+    int32_t max_blocks;          /* paged: columns of block_table */
+    int32_t num_blocks;          /* physical pages; contiguous: sequences */
+    int32_t capacity;            /* contiguous: token rows per sequence */
+    int32_t reserved;            /* must be 0 */
+} spire_latent;
+
+/*
+ * The projections of N tokens on their way into a latent cache, in one pass:
+ * the latent is normed, the shared key part and the queries' position parts
+ * are rotated; [latent, key part] goes to the token's slot, the queries' parts
+ * into the last Dr elements of the absorbed queries' rows.
+ *   c_new [N, Dc], k_rope [N, Dr], q_rope [N, Hq, Dr]: in_dtype SPIRE_F32 or
+ *     SPIRE_BF16; tokens c_stride / k_stride / q_stride elements apart, heads
+ *     q_head_stride.  Hq = 0: no queries (q_rope and q_out unused).
+ *   weight [Dc] fp32 or NULL (no norm); eps >= 0; rope->rot_dim == Dr, or NULL.
+ *   q_out [N, Hq, Dc + Dr] contiguous, out_dtype SPIRE_F32 or SPIRE_BF16: elements
+ *     Dc .. Dc + Dr - 1 of every row are written, the others left alone.
+ *   sizes  0 <= N < 2^31, 0 <= Hq <= 4096, 1 <= Dc <= 4096, 1 <= Dr <= 1024.
+ * Slots, rounding and overlap as for spire_qkv_append.  No workspace.
+ */
+spire_status spire_latent_append(const void *c_new, int64_t c_stride, const void *k_rope,
+                                 int64_t k_stride, const void *q_rope, int64_t q_stride,
+                                 int64_t q_head_stride, int32_t in_dtype, const float *weight,
+                                 float eps, const spire_rope *rope, const spire_latent *latent,
+                                 const int64_t *slots, int32_t N, int32_t Hq, void *q_out,
+                                 int32_t out_dtype, hipStream_t stream);
+
+/* Bytes of workspace spire_latent_verify_attn needs for these sizes on the
+ * current device (0 on invalid sizes). */
+size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc);
+
+/*
+ * Target verification attention over a latent cache, absorbed form: the
+ * queries have been brought into the latent's space, so every head reads the
+ * same rows, as key (all Dc + Dr elements) and as value (the first Dc).
+ *   q        [B, k+1, Hq, Dc + Dr] contiguous, q_dtype SPIRE_F32 or SPIRE_BF16.
+ *   latent   the cache, the round's tokens appended; kv_lens [B], the mask, empty
+ *            rows and lengths beyond the storage as for spire_verify_attn (k = 0:
+ *            one new token a sequence).
+ *   s = sm_scale * <q, row>; out [B, k+1, Hq, Dc] = sum softmax(s) latent, out_dtype
+ *            SPIRE_F32 or SPIRE_BF16; lse [B, k+1, Hq] fp32 natural log, or NULL.
+ *   sizes    0 <= B <= 8192, 1 <= Hq <= 128, 0 <= k <= 15, Dc 256 or 512, Dr = 64
+ *            (SPIRE_ERR_UNSUPPORTED otherwise).
+ *   workspace >= spire_latent_workspace_size(B, Hq, k, Dc) bytes, 256-byte aligned.
+ * bf16 queries on bf16 or fp8 caches whose rows start 16-byte aligned run on the
+ * 16-bit matrix instructions (probabilities rounded to 16 bits, sums in fp32),
+ * everything else in fp32.  Non-finite values act as for spire_verify_attn;
+ * a key that a row does not see never influences it, whatever it holds.
+ */
+spire_status spire_latent_verify_attn(const void *q, int32_t q_dtype, const spire_latent *latent,
+                                      const int32_t *kv_lens, int32_t B, int32_t Hq, int32_t k,
+                                      float sm_scale, void *out, int32_t out_dtype, float *lse,
+                                      void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
  * Streaming-read probe (a measurement aid, not a step of the method): reads
  * the `bytes` bytes at device pointer `buf` once with 16-byte nontemporal
  * loads, as a plain streaming kernel does, and writes an XOR fold of what it
@@ -384,7 +562,7 @@ int32_t spire_version(void);
 /*
  * Per-call options of the entry points that launch several kernels
  * (spire_verify_attn_ex, spire_draft_sparse_attn_ex, spire_token_verify_ex,
- * spire_block_verify_ex).
+ * spire_block_verify_ex, spire_latent_verify_attn_ex).
  * A NULL pointer, or a zero-initialised struct, means the defaults; the
  * library reads the struct and writes the host arrays it points to only
  * during the call and keeps nothing afterwards, so calls stay reentrant.
@@ -423,7 +601,8 @@ int32_t spire_version(void);
  *                 the fp32 matrix kernels), 4 token verification weights,
  *                 5 token verification select, 11 the check of the values of
  *                 keys [n - k, n) after a matrix-core verify call, 12 block
- *                 verification weights, 13 block verification select.
+ *                 verification weights, 13 block verification select, 14 latent
+ *                 attention, 15 latent combine.
  *   n_launches    host int32 or NULL: set to the number of kernels the call
  *                 launched (0 when it returned before launching).
  *   reserved      must be 0.
@@ -463,6 +642,12 @@ spire_status spire_block_verify_ex(const float *p_target, const float *q_draft,
                                    int32_t *n_accepted, int32_t *out_tokens, void *workspace,
                                    size_t workspace_bytes, hipStream_t stream,
                                    const spire_launch_opts *opts);
+/* opts->kernel: 0 automatic, 1 always the fp32 kernel, 2 and 3 as 0. */
+spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const spire_latent *latent,
+                                         const int32_t *kv_lens, int32_t B, int32_t Hq, int32_t k,
+                                         float sm_scale, void *out, int32_t out_dtype, float *lse,
+                                         void *workspace, size_t workspace_bytes, hipStream_t stream,
+                                         const spire_launch_opts *opts);
 
 #ifdef __cplusplus
 }

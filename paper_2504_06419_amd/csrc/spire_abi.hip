@@ -117,7 +117,8 @@ size_t workspace_bytes_for(int B, int R, int D) {
 // ---- per-call options: kernel family and launch events ----------------------------
 // Kernel ids of the recorded launches (include/spire.h).
 enum { KID_PLAN = 0, KID_VERIFY = 1, KID_DRAFT = 2, KID_COMBINE = 3, KID_TOKEN_WEIGHTS = 4,
-       KID_TOKEN_SELECT = 5, KID_TAIL_CHECK = 11, KID_BLOCK_WEIGHTS = 12, KID_BLOCK_SELECT = 13 };
+       KID_TOKEN_SELECT = 5, KID_TAIL_CHECK = 11, KID_BLOCK_WEIGHTS = 12, KID_BLOCK_SELECT = 13,
+       KID_LATENT = 14, KID_LATENT_COMBINE = 15 };
 
 // Records the caller's events around each launch of one call, in launch order.
 struct Recorder {
@@ -816,6 +817,320 @@ spire_status spire_draft_rollback(const spire_kv *sink, const spire_kv *ring, co
     hipError_t e = launch_draft_rollback(ds, dr, spill_k, spill_v, base_lens, n_accepted, steps, ring_offset, B,
                                          Hkv, D, S, W, stream);
     if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "draft rollback launch: %s", hipGetErrorString(e));
+    return SPIRE_OK;
+}
+
+// ---- pages ---------------------------------------------------------------------
+
+size_t spire_page_workspace_size(int32_t B) {
+    return B < 0 || B > kPlanMaxB ? 0 : align256(page_workspace_bytes(B));
+}
+
+static spire_status check_pages(const void *table, int32_t page_size, int32_t max_blocks, const void *lens,
+                                const void *change, int32_t B, const void *free_pages, int32_t pool,
+                                const void *n_free, const void *lens_out, const void *n_free_out,
+                                const void *workspace, size_t workspace_bytes) {
+    if (B < 0 || pool < 0) return fail(SPIRE_ERR_INVALID_ARG, "need B >= 0 and pool >= 0");
+    if (B > kPlanMaxB) return fail(SPIRE_ERR_UNSUPPORTED, "B must be <= %d (got %d)", kPlanMaxB, B);
+    if (page_size < 1 || max_blocks < 1) return fail(SPIRE_ERR_INVALID_ARG, "need page_size >= 1 and max_blocks >= 1");
+    if (n_free == nullptr || n_free_out == nullptr) return fail(SPIRE_ERR_INVALID_ARG, "n_free or n_free_out is NULL");
+    if (B > 0 && (table == nullptr || lens == nullptr || change == nullptr || lens_out == nullptr))
+        return fail(SPIRE_ERR_INVALID_ARG, "block_table, lens, new_tokens / keep or lens_out is NULL");
+    if (pool > 0 && free_pages == nullptr) return fail(SPIRE_ERR_INVALID_ARG, "free_pages is NULL");
+    for (const void *ptr : {table, lens, change, free_pages, n_free, lens_out, n_free_out})
+        if (((uintptr_t)ptr & 3u) != 0) return fail(SPIRE_ERR_INVALID_ARG, "arrays must be 4-byte aligned");
+    if (workspace == nullptr) return fail(SPIRE_ERR_WORKSPACE, "workspace is NULL");
+    if (((uintptr_t)workspace & 255u) != 0) return fail(SPIRE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    const size_t need = spire_page_workspace_size(B);
+    if (workspace_bytes < need)
+        return fail(SPIRE_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, need);
+    return SPIRE_OK;
+}
+
+spire_status spire_page_extend(int32_t *block_table, int32_t page_size, int32_t max_blocks,
+                               const int32_t *lens, const int32_t *new_tokens, int32_t B,
+                               const int32_t *free_pages, int32_t pool, const int32_t *n_free,
+                               int64_t *slots, int32_t *positions, int32_t max_tokens,
+                               int32_t *cu_tokens, int32_t *lens_out, int32_t *n_free_out,
+                               void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    g_err[0] = '\0';
+    const spire_status s = check_pages(block_table, page_size, max_blocks, lens, new_tokens, B, free_pages, pool,
+                                       n_free, lens_out, n_free_out, workspace, workspace_bytes);
+    if (s != SPIRE_OK) return s;
+    if (max_tokens < 0 || max_tokens > (1 << 30))
+        return fail(SPIRE_ERR_INVALID_ARG, "max_tokens must be in [0, 2^30] (got %d)", max_tokens);
+    if (max_tokens > 0 && (slots == nullptr || positions == nullptr))
+        return fail(SPIRE_ERR_INVALID_ARG, "slots or positions is NULL");
+    if (cu_tokens == nullptr) return fail(SPIRE_ERR_INVALID_ARG, "cu_tokens is NULL");
+    if (((uintptr_t)slots & 7u) != 0 || ((uintptr_t)positions & 3u) != 0 || ((uintptr_t)cu_tokens & 3u) != 0)
+        return fail(SPIRE_ERR_INVALID_ARG, "slots, positions and cu_tokens must be aligned to their elements");
+    const PageExtend x{block_table, lens, new_tokens, free_pages, n_free, slots, positions, cu_tokens, lens_out,
+                       n_free_out, B, page_size, max_blocks, pool, max_tokens, workspace};
+    const hipError_t e = launch_page_extend(x, stream);
+    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "page extend launch: %s", hipGetErrorString(e));
+    return SPIRE_OK;
+}
+
+spire_status spire_page_release(const int32_t *block_table, int32_t page_size, int32_t max_blocks,
+                                const int32_t *lens, const int32_t *keep, int32_t B,
+                                int32_t *free_pages, int32_t pool, const int32_t *n_free,
+                                int32_t *lens_out, int32_t *n_free_out, void *workspace,
+                                size_t workspace_bytes, hipStream_t stream) {
+    g_err[0] = '\0';
+    const spire_status s = check_pages(block_table, page_size, max_blocks, lens, keep, B, free_pages, pool, n_free,
+                                       lens_out, n_free_out, workspace, workspace_bytes);
+    if (s != SPIRE_OK) return s;
+    const PageRelease x{block_table, lens, keep, free_pages, n_free, lens_out, n_free_out, B, page_size, max_blocks,
+                        pool, workspace};
+    const hipError_t e = launch_page_release(x, stream);
+    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "page release launch: %s", hipGetErrorString(e));
+    return SPIRE_OK;
+}
+
+// ---- appends with norms and rotation ----------------------------------------------
+
+static spire_status check_rope(const spire_rope *r, int32_t D, bool all) {
+    if (r == nullptr) return SPIRE_OK;
+    if (r->reserved != 0) return fail(SPIRE_ERR_INVALID_ARG, "rope: reserved field must be 0");
+    if (r->rot_dim < 0 || r->rot_dim % 2 != 0 || r->rot_dim > D)
+        return fail(SPIRE_ERR_INVALID_ARG, "rope: rot_dim must be even and in [0, %d] (got %d)", D, r->rot_dim);
+    if (all && r->rot_dim != D) return fail(SPIRE_ERR_INVALID_ARG, "rope: rot_dim must be %d (got %d)", D, r->rot_dim);
+    if (r->axes < 1 || r->axes > 8) return fail(SPIRE_ERR_UNSUPPORTED, "rope: axes must be in [1, 8] (got %d)", r->axes);
+    if (r->interleaved != 0 && r->interleaved != 1) return fail(SPIRE_ERR_INVALID_ARG, "rope: interleaved must be 0 or 1");
+    if (r->rot_dim > 0 && (r->positions == nullptr || r->inv_freq == nullptr))
+        return fail(SPIRE_ERR_INVALID_ARG, "rope: positions or inv_freq is NULL");
+    for (const void *ptr : {(const void *)r->positions, (const void *)r->inv_freq, (const void *)r->axis})
+        if (((uintptr_t)ptr & 3u) != 0) return fail(SPIRE_ERR_INVALID_ARG, "rope: arrays must be 4-byte aligned");
+    return SPIRE_OK;
+}
+
+// types of an append's inputs and of the queries it writes
+static spire_status check_append(int32_t in_dtype, int32_t out_dtype, float eps, const void *slots, int32_t N) {
+    if (N < 0) return fail(SPIRE_ERR_INVALID_ARG, "N must be >= 0 (got %d)", N);
+    if (in_dtype != SPIRE_F32 && in_dtype != SPIRE_BF16) return fail(SPIRE_ERR_UNSUPPORTED, "in_dtype must be F32 or BF16");
+    if (out_dtype != SPIRE_F32 && out_dtype != SPIRE_BF16)
+        return fail(SPIRE_ERR_UNSUPPORTED, "out_dtype must be F32 or BF16");
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(SPIRE_ERR_INVALID_ARG, "eps must be finite and >= 0");
+    if (N > 0 && slots == nullptr) return fail(SPIRE_ERR_INVALID_ARG, "slots is NULL");
+    if (((uintptr_t)slots & 7u) != 0) return fail(SPIRE_ERR_INVALID_ARG, "slots must be 8-byte aligned");
+    return SPIRE_OK;
+}
+
+static bool on_elements(const void *p, int dtype) { return ((uintptr_t)p & (dtype == SPIRE_F32 ? 3u : 1u)) == 0; }
+
+spire_status spire_qkv_append(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                              const void *v, int64_t v_stride, int32_t in_dtype,
+                              const float *q_weight, const float *k_weight, float eps,
+                              const spire_rope *rope, const spire_kv *kv, const int64_t *slots,
+                              int32_t N, int32_t Hq, int32_t Hkv, int32_t D, void *q_out,
+                              int32_t out_dtype, hipStream_t stream) {
+    g_err[0] = '\0';
+    if (Hq < 1 || Hkv < 1) return fail(SPIRE_ERR_INVALID_ARG, "need Hq >= 1 and Hkv >= 1");
+    if ((int64_t)Hq + 2 * (int64_t)Hkv > 4096) return fail(SPIRE_ERR_UNSUPPORTED, "Hq + 2 Hkv must be <= 4096");
+    if (D < 1 || D > 1024) return fail(SPIRE_ERR_UNSUPPORTED, "D must be in [1, 1024] (got %d)", D);
+    spire_status s = check_append(in_dtype, out_dtype, eps, slots, N);
+    if (s != SPIRE_OK) return s;
+    s = check_rope(rope, D, false);
+    if (s != SPIRE_OK) return s;
+    s = check_kv(kv, "kv", D, Hkv, true);
+    if (s != SPIRE_OK) return s;
+    if (kv->page_size == 0 && kv->num_blocks < 0) return fail(SPIRE_ERR_INVALID_ARG, "kv: negative num_blocks");
+    if (!elems_aligned(kv)) return fail(SPIRE_ERR_INVALID_ARG, "kv storage not aligned to its element size");
+    if (q_stride < 0 || k_stride < 0 || v_stride < 0) return fail(SPIRE_ERR_INVALID_ARG, "negative token stride");
+    if (N == 0) return SPIRE_OK;
+    if (q == nullptr || k == nullptr || v == nullptr || q_out == nullptr)
+        return fail(SPIRE_ERR_INVALID_ARG, "q, k, v or q_out is NULL");
+    if (!on_elements(q, in_dtype) || !on_elements(k, in_dtype) || !on_elements(v, in_dtype) ||
+        !on_elements(q_out, out_dtype) || !on_elements(q_weight, SPIRE_F32) || !on_elements(k_weight, SPIRE_F32))
+        return fail(SPIRE_ERR_INVALID_ARG, "arrays must be aligned to their element size");
+    const QkvAppend x{q, k, v, q_stride, k_stride, v_stride, q_weight, k_weight, rope, to_dev(kv), slots, q_out, eps,
+                      in_dtype, out_dtype, N, Hq, Hkv, D};
+    const hipError_t e = launch_qkv_append(x, stream);
+    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "qkv append launch: %s", hipGetErrorString(e));
+    return SPIRE_OK;
+}
+
+static spire_status check_latent(const spire_latent *c) {
+    if (c == nullptr) return fail(SPIRE_ERR_INVALID_ARG, "latent: descriptor is NULL");
+    if (c->c == nullptr) return fail(SPIRE_ERR_INVALID_ARG, "latent: c is NULL");
+    const int es = elem_size(c->dtype);
+    if (es == 0) return fail(SPIRE_ERR_INVALID_ARG, "latent: unknown dtype %d", c->dtype);
+    if (c->reserved != 0) return fail(SPIRE_ERR_INVALID_ARG, "latent: reserved field must be 0");
+    if (c->Dc < 1 || c->Dc > 4096 || c->Dr < 1 || c->Dr > 1024)
+        return fail(SPIRE_ERR_UNSUPPORTED, "latent: Dc must be in [1, 4096] and Dr in [1, 1024] (got %d, %d)", c->Dc, c->Dr);
+    if (c->s_blk < 0 || c->s_tok < 0) return fail(SPIRE_ERR_INVALID_ARG, "latent: negative stride");
+    if (c->dtype == SPIRE_FP8_E4M3FN && c->scale == nullptr)
+        return fail(SPIRE_ERR_INVALID_ARG, "latent: fp8 storage needs a scale");
+    if (c->page_size < 0 || c->num_blocks < 0 || c->capacity < 0)
+        return fail(SPIRE_ERR_INVALID_ARG, "latent: negative page_size, num_blocks or capacity");
+    if ((uintptr_t)c->c % es != 0) return fail(SPIRE_ERR_INVALID_ARG, "latent: storage not aligned to its element size");
+    return SPIRE_OK;
+}
+
+static KvDev latent_dev(const spire_latent *c) {
+    KvDev d;
+    d.k = static_cast<const uint8_t *>(c->c);
+    d.v = nullptr;
+    d.block_table = c->block_table;
+    d.k_scale = c->scale;
+    d.v_scale = nullptr;
+    d.s_blk = c->s_blk;
+    d.s_head = 0;
+    d.s_tok = c->s_tok;
+    d.elem = elem_size(c->dtype);
+    d.page_size = c->page_size;
+    d.max_blocks = c->max_blocks;
+    d.num_blocks = c->num_blocks;
+    d.capacity = c->capacity;
+    return d;
+}
+
+spire_status spire_latent_append(const void *c_new, int64_t c_stride, const void *k_rope,
+                                 int64_t k_stride, const void *q_rope, int64_t q_stride,
+                                 int64_t q_head_stride, int32_t in_dtype, const float *weight,
+                                 float eps, const spire_rope *rope, const spire_latent *latent,
+                                 const int64_t *slots, int32_t N, int32_t Hq, void *q_out,
+                                 int32_t out_dtype, hipStream_t stream) {
+    g_err[0] = '\0';
+    if (Hq < 0) return fail(SPIRE_ERR_INVALID_ARG, "Hq must be >= 0 (got %d)", Hq);
+    if (Hq > 4096) return fail(SPIRE_ERR_UNSUPPORTED, "Hq must be <= 4096 (got %d)", Hq);
+    spire_status s = check_append(in_dtype, out_dtype, eps, slots, N);
+    if (s != SPIRE_OK) return s;
+    s = check_latent(latent);
+    if (s != SPIRE_OK) return s;
+    s = check_rope(rope, latent->Dr, true);
+    if (s != SPIRE_OK) return s;
+    if (c_stride < 0 || k_stride < 0 || q_stride < 0 || q_head_stride < 0)
+        return fail(SPIRE_ERR_INVALID_ARG, "negative stride");
+    if (N == 0) return SPIRE_OK;
+    if (c_new == nullptr || k_rope == nullptr || (Hq > 0 && (q_rope == nullptr || q_out == nullptr)))
+        return fail(SPIRE_ERR_INVALID_ARG, "c_new, k_rope, q_rope or q_out is NULL");
+    if (!on_elements(c_new, in_dtype) || !on_elements(k_rope, in_dtype) || !on_elements(q_rope, in_dtype) ||
+        !on_elements(q_out, out_dtype) || !on_elements(weight, SPIRE_F32))
+        return fail(SPIRE_ERR_INVALID_ARG, "arrays must be aligned to their element size");
+    const LatentAppend x{c_new, k_rope, q_rope, c_stride, k_stride, q_stride, q_head_stride, weight, rope,
+                         latent_dev(latent), slots, q_out, eps, in_dtype, out_dtype, N, Hq, latent->Dc, latent->Dr};
+    const hipError_t e = launch_latent_append(x, stream);
+    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "latent append launch: %s", hipGetErrorString(e));
+    return SPIRE_OK;
+}
+
+// ---- latent attention ----------------------------------------------------------
+
+// Blocks per unit and groups of a launch (latent_common.h).
+struct LatentShape { int nb, units, groups; };
+
+static LatentShape latent_shape(int Hq, int k, int cus) {
+    const int blocks = (k + 1) * ((Hq + 15) / 16);
+    LatentShape s;
+    s.nb = 1;
+    s.units = blocks;
+    s.groups = std::max(1, cus / s.units);
+    return s;
+}
+
+static Layout latent_layout(int B, int Dc, const LatentShape &s) {
+    return layout(B, (int64_t)s.units * s.nb * 16, Dc, s.groups);
+}
+
+size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc) {
+    if (B < 0 || B > kPlanMaxB || Hq < 1 || Hq > 128 || k < 0 || k > 15 || (Dc != 256 && Dc != 512)) return 0;
+    int cus = 0;
+    if (device_cus(&cus) != 0) return 0;
+    return latent_layout(B, Dc, latent_shape(Hq, k, cus)).total;
+}
+
+spire_status spire_latent_verify_attn(const void *q, int32_t q_dtype, const spire_latent *latent,
+                                      const int32_t *kv_lens, int32_t B, int32_t Hq, int32_t k,
+                                      float sm_scale, void *out, int32_t out_dtype, float *lse,
+                                      void *workspace, size_t workspace_bytes, hipStream_t stream) {
+    return spire_latent_verify_attn_ex(q, q_dtype, latent, kv_lens, B, Hq, k, sm_scale, out, out_dtype, lse,
+                                       workspace, workspace_bytes, stream, nullptr);
+}
+
+spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const spire_latent *latent,
+                                         const int32_t *kv_lens, int32_t B, int32_t Hq, int32_t k,
+                                         float sm_scale, void *out, int32_t out_dtype, float *lse,
+                                         void *workspace, size_t workspace_bytes, hipStream_t stream,
+                                         const spire_launch_opts *opts) {
+    g_err[0] = '\0';
+    if (opts != nullptr && opts->n_launches != nullptr) *opts->n_launches = 0;
+    spire_status s = check_opts(opts);
+    if (s != SPIRE_OK) return s;
+    if (B < 0) return fail(SPIRE_ERR_INVALID_ARG, "B must be >= 0 (got %d)", B);
+    if (B > kPlanMaxB) return fail(SPIRE_ERR_UNSUPPORTED, "B must be <= %d (got %d)", kPlanMaxB, B);
+    if (Hq < 1) return fail(SPIRE_ERR_INVALID_ARG, "Hq must be >= 1 (got %d)", Hq);
+    if (Hq > 128) return fail(SPIRE_ERR_UNSUPPORTED, "Hq must be <= 128 (got %d)", Hq);
+    if (k < 0 || k > 15) return fail(SPIRE_ERR_UNSUPPORTED, "k must be in [0, 15] (got %d)", k);
+    if (q_dtype != SPIRE_F32 && q_dtype != SPIRE_BF16) return fail(SPIRE_ERR_UNSUPPORTED, "q_dtype must be F32 or BF16");
+    if (out_dtype != SPIRE_F32 && out_dtype != SPIRE_BF16)
+        return fail(SPIRE_ERR_UNSUPPORTED, "out_dtype must be F32 or BF16");
+    s = check_scale(sm_scale);
+    if (s != SPIRE_OK) return s;
+    s = check_latent(latent);
+    if (s != SPIRE_OK) return s;
+    if ((latent->Dc != 256 && latent->Dc != 512) || latent->Dr != kLatentDr)
+        return fail(SPIRE_ERR_UNSUPPORTED, "latent attention takes Dc 256 or 512 and Dr %d (got %d, %d)", kLatentDr,
+                    latent->Dc, latent->Dr);
+    if (latent->page_size > 0 ? latent->block_table == nullptr || latent->max_blocks <= 0 || latent->num_blocks <= 0
+                              : latent->capacity <= 0 && B > 0)
+        return fail(SPIRE_ERR_INVALID_ARG, "latent: a paged view needs block_table, max_blocks > 0 and num_blocks > 0, "
+                                           "a contiguous one capacity > 0");
+    if (((uintptr_t)latent->block_table & 3u) != 0 || ((uintptr_t)latent->scale & 3u) != 0 ||
+        ((uintptr_t)kv_lens & 3u) != 0 || ((uintptr_t)lse & 3u) != 0)
+        return fail(SPIRE_ERR_INVALID_ARG, "block_table, scale, kv_lens and lse must be 4-byte aligned");
+    if (B == 0) return SPIRE_OK;
+    if (q == nullptr || out == nullptr || kv_lens == nullptr)
+        return fail(SPIRE_ERR_INVALID_ARG, "q, out or kv_lens is NULL");
+    if (!aligned16(q) || !aligned16(out)) return fail(SPIRE_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+    if (workspace == nullptr) return fail(SPIRE_ERR_WORKSPACE, "workspace is NULL");
+    if (((uintptr_t)workspace & 255u) != 0) return fail(SPIRE_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+    int cus = 0;
+    if (device_cus(&cus) != 0) return fail(SPIRE_ERR_HIP, "cannot query the current HIP device");
+
+    Latent a;
+    memset(&a, 0, sizeof a);
+    Problem &p = a.p;
+    p.B = B; p.Hq = Hq; p.Hkv = 1; p.D = latent->Dc; p.k = k;
+    p.g = Hq;
+    p.R = (k + 1) * Hq;
+    p.sm_scale_log2 = sm_scale * 1.4426950408889634f;
+    p.q = static_cast<const uint8_t *>(q);
+    p.q_dtype = q_dtype;
+    p.kv_dtype = latent->dtype;
+    p.lens = kv_lens;
+    p.kv = latent_dev(latent);
+    p.out = out;
+    p.out_dtype = out_dtype;
+    p.lse = lse;
+    const LatentShape sh = latent_shape(Hq, k, cus);
+    a.hb = (Hq + 15) / 16;
+    a.nb = sh.nb;
+    a.units = sh.units;
+    const int es = p.kv.elem;
+    a.quads = (uintptr_t)latent->c % (4 * es) == 0 && latent->s_blk % 4 == 0 && latent->s_tok % 4 == 0;
+    Plan &pl = a.pl;
+    pl.tile = 32;
+    pl.units = 1;
+    pl.rows = sh.units * sh.nb * 16;
+    pl.workers = sh.groups;
+    pl.seg_cost = 0;
+    const Layout L = latent_layout(B, p.D, sh);
+    if (workspace_bytes < L.total)
+        return fail(SPIRE_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, L.total);
+    char *ws = static_cast<char *>(workspace);
+    pl.nkeys = reinterpret_cast<int32_t *>(ws + L.nkeys);
+    pl.prefix = reinterpret_cast<int32_t *>(ws + L.prefix);
+    pl.wstart = reinterpret_cast<int32_t *>(ws + L.wstart);
+    pl.part_lse = reinterpret_cast<float *>(ws + L.part_lse);
+    pl.part_o = reinterpret_cast<float *>(ws + L.part_o);
+    Recorder rec(opts);
+    hipError_t e = rec.run(KID_PLAN, stream, launch_plan, p, pl);
+    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "plan launch: %s", hipGetErrorString(e));
+    e = rec.run(KID_LATENT, stream, [&] { return launch_latent_f32(a, stream); });
+    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "latent attention launch: %s", hipGetErrorString(e));
+    e = rec.run(KID_LATENT_COMBINE, stream, [&] { return launch_latent_combine(a, stream); });
+    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "latent combine launch: %s", hipGetErrorString(e));
     return SPIRE_OK;
 }
 

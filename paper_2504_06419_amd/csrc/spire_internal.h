@@ -267,6 +267,66 @@ struct FeedbackArgs {
 };
 hipError_t launch_feedback_memory(const FeedbackArgs &a, hipStream_t st);
 
+// ---- pages (pages.hip) ----------------------------------------------------------
+struct PageExtend {
+    int32_t *table;
+    const int32_t *lens, *new_tokens, *free_pages, *n_free;
+    int64_t *slots;
+    int32_t *positions, *cu, *lens_out, *n_free_out;
+    int32_t B, page_size, max_blocks, pool, max_tokens;
+    void *ws;
+};
+struct PageRelease {
+    const int32_t *table, *lens, *keep;
+    int32_t *free_pages;
+    const int32_t *n_free;
+    int32_t *lens_out, *n_free_out;
+    int32_t B, page_size, max_blocks, pool;
+    void *ws;
+};
+size_t page_workspace_bytes(int B);
+hipError_t launch_page_extend(const PageExtend &x, hipStream_t st);
+hipError_t launch_page_release(const PageRelease &x, hipStream_t st);
+
+// ---- appends with norms and rotation (rope_append.hip) ----------------------------
+struct QkvAppend {
+    const void *q, *k, *v;
+    int64_t q_stride, k_stride, v_stride;
+    const float *q_weight, *k_weight;
+    const spire_rope *rope;  // host struct or null
+    KvDev kv;
+    const int64_t *slots;
+    void *q_out;
+    float eps;
+    int32_t in_dtype, out_dtype, N, Hq, Hkv, D;
+};
+struct LatentAppend {
+    const void *c, *k, *q;
+    int64_t c_stride, k_stride, q_stride, q_head_stride;
+    const float *weight;
+    const spire_rope *rope;
+    KvDev kv;                // of the latent view: k, k_scale, s_blk, s_tok
+    const int64_t *slots;
+    void *q_out;
+    float eps;
+    int32_t in_dtype, out_dtype, N, Hq, Dc, Dr;
+};
+hipError_t launch_qkv_append(const QkvAppend &x, hipStream_t st);
+hipError_t launch_latent_append(const LatentAppend &x, hipStream_t st);
+
+// ---- latent attention (latent_common.h, latent_attn.hip) ----------------------------
+constexpr int kLatentDr = 64;  // rotated elements of a row
+struct Latent {
+    Problem p;        // Hkv = 1, D = Dc, kv = the latent view (k, k_scale)
+    Plan pl;          // units = 1: positions of one row of segments; workers: groups
+    int32_t hb;       // 16-row blocks per query token
+    int32_t nb;       // blocks per unit
+    int32_t units;    // units per sequence = workgroups per group
+    int32_t quads;    // fp32 kernel: cache elements readable four at a time
+};
+hipError_t launch_latent_f32(const Latent &a, hipStream_t st);
+hipError_t launch_latent_combine(const Latent &a, hipStream_t st);
+
 // MFMA kernel tile size (keys) and its worker count per CU.
 constexpr int kMfmaTile = 32;
 constexpr int kMfmaWavesPerWG = 4;

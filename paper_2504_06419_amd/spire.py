@@ -28,14 +28,16 @@ SYMBOLS = ["spire_verify_workspace_size", "spire_verify_attn", "spire_verify_att
            "spire_draft_sparse_attn", "spire_token_verify_workspace_size", "spire_token_verify",
            "spire_block_verify_workspace_size", "spire_block_verify",
            "spire_kv_append", "spire_draft_append", "spire_draft_rollback", "spire_feedback_memory",
+           "spire_page_workspace_size", "spire_page_extend", "spire_page_release", "spire_qkv_append",
+           "spire_latent_append", "spire_latent_workspace_size", "spire_latent_verify_attn",
            "spire_hbm_read_probe", "spire_status_string", "spire_last_error", "spire_version",
            "spire_verify_attn_ex", "spire_draft_sparse_attn_ex", "spire_token_verify_ex",
-           "spire_block_verify_ex"]
+           "spire_block_verify_ex", "spire_latent_verify_attn_ex"]
 
 # kernel ids of the launches recorded through spire_launch_opts
 KERNEL_IDS = {0: "plan", 1: "verify_partial", 2: "draft_partial", 3: "combine",
               4: "token_weights", 5: "token_select", 11: "tail_check", 12: "block_weights",
-              13: "block_select"}
+              13: "block_select", 14: "latent_attn", 15: "latent_combine"}
 # kernel families (spire_launch_opts.kernel)
 KERNEL_AUTO, KERNEL_GENERIC, KERNEL_REGS, KERNEL_LDS = 0, 1, 2, 3
 HBM_PROBE_SINK_WORDS = 2048
@@ -60,6 +62,21 @@ class LaunchOpts(C.Structure):
     """struct spire_launch_opts"""
     _fields_ = [("kernel", C.c_int32), ("max_launches", C.c_int32), ("events", C.c_void_p),
                 ("kernel_ids", C.c_void_p), ("n_launches", C.c_void_p), ("reserved", C.c_int32)]
+
+
+class Rope(C.Structure):
+    """struct spire_rope"""
+    _fields_ = [("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("axis", C.c_void_p),
+                ("axes", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class Latent(C.Structure):
+    """struct spire_latent"""
+    _fields_ = [("c", C.c_void_p), ("block_table", C.c_void_p), ("scale", C.c_void_p),
+                ("s_blk", C.c_int64), ("s_tok", C.c_int64), ("dtype", C.c_int32), ("Dc", C.c_int32),
+                ("Dr", C.c_int32), ("page_size", C.c_int32), ("max_blocks", C.c_int32),
+                ("num_blocks", C.c_int32), ("capacity", C.c_int32), ("reserved", C.c_int32)]
 
 
 _lib = None
@@ -119,6 +136,25 @@ def load(path: Optional[str] = None):
     L.spire_block_verify.argtypes = L.spire_token_verify.argtypes
     L.spire_block_verify_ex.restype = C.c_int
     L.spire_block_verify_ex.argtypes = L.spire_token_verify.argtypes + [C.POINTER(LaunchOpts)]
+    i64, f32 = C.c_int64, C.c_float
+    L.spire_page_workspace_size.restype = sz
+    L.spire_page_workspace_size.argtypes = [i32]
+    L.spire_page_extend.restype = C.c_int
+    L.spire_page_extend.argtypes = [vp, i32, i32, vp, vp, i32, vp, i32, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    L.spire_page_release.restype = C.c_int
+    L.spire_page_release.argtypes = [vp, i32, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp, sz, vp]
+    L.spire_qkv_append.restype = C.c_int
+    L.spire_qkv_append.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, vp, f32, C.POINTER(Rope), C.POINTER(KV), vp,
+                                   i32, i32, i32, i32, vp, i32, vp]
+    L.spire_latent_append.restype = C.c_int
+    L.spire_latent_append.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, vp, f32, C.POINTER(Rope),
+                                      C.POINTER(Latent), vp, i32, i32, vp, i32, vp]
+    L.spire_latent_workspace_size.restype = sz
+    L.spire_latent_workspace_size.argtypes = [i32] * 4
+    L.spire_latent_verify_attn.restype = C.c_int
+    L.spire_latent_verify_attn.argtypes = [vp, i32, C.POINTER(Latent), vp, i32, i32, i32, f32, vp, i32, vp, vp, sz, vp]
+    L.spire_latent_verify_attn_ex.restype = C.c_int
+    L.spire_latent_verify_attn_ex.argtypes = L.spire_latent_verify_attn.argtypes + [C.POINTER(LaunchOpts)]
     L.spire_hbm_read_probe.restype = C.c_int
     L.spire_hbm_read_probe.argtypes = [vp, sz, vp, sz, vp]
     if path is None:
@@ -170,6 +206,7 @@ def kv_view(k: torch.Tensor, v: torch.Tensor, block_table: Optional[torch.Tensor
     else:
         kv.block_table = None
         kv.page_size = 0
+        kv.num_blocks = k.shape[0]
         kv.capacity = k.shape[2] if capacity is None else capacity
     kv.reserved = 0
     return kv
@@ -395,6 +432,170 @@ def feedback_memory(x: torch.Tensor, w: torch.Tensor, out: Optional[torch.Tensor
     _check(load().spire_feedback_memory(x.data_ptr(), _DT[x.dtype], w.data_ptr(), n_out, layers, B, d,
                                         out.data_ptr(), _DT[out.dtype], _stream()))
     return out
+
+
+def page_workspace_size(B) -> int:
+    return int(load().spire_page_workspace_size(B))
+
+
+def _ints(*tensors):
+    for t in tensors:
+        assert t.dtype == torch.int32 and t.is_contiguous()
+
+
+def page_extend(block_table: torch.Tensor, page_size: int, lens: torch.Tensor, new_tokens: torch.Tensor,
+                free_pages: torch.Tensor, n_free: torch.Tensor, slots: torch.Tensor, positions: torch.Tensor,
+                cu_tokens: torch.Tensor, lens_out: Optional[torch.Tensor] = None,
+                n_free_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """spire_page_extend.  block_table [B, max_blocks], lens / new_tokens [B], free_pages [pool], n_free [1]
+    int32; slots [max_tokens] int64, positions [max_tokens], cu_tokens [B + 1] int32 are written; lens and
+    n_free are updated in place unless lens_out / n_free_out are given."""
+    B, max_blocks = block_table.shape
+    lens_out = lens if lens_out is None else lens_out
+    n_free_out = n_free if n_free_out is None else n_free_out
+    _ints(block_table, lens, new_tokens, free_pages, n_free, positions, cu_tokens, lens_out, n_free_out)
+    assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == positions.numel()
+    assert lens.numel() == B and new_tokens.numel() == B and lens_out.numel() == B and cu_tokens.numel() == B + 1
+    if ws is None:
+        ws = workspace(page_workspace_size(B), lens.device)
+    _check(load().spire_page_extend(block_table.data_ptr(), page_size, max_blocks, lens.data_ptr(),
+                                    new_tokens.data_ptr(), B, free_pages.data_ptr(), free_pages.numel(),
+                                    n_free.data_ptr(), slots.data_ptr(), positions.data_ptr(), slots.numel(),
+                                    cu_tokens.data_ptr(), lens_out.data_ptr(), n_free_out.data_ptr(),
+                                    ws.data_ptr(), ws.numel(), _stream()))
+
+
+def page_release(block_table: torch.Tensor, page_size: int, lens: torch.Tensor, keep: torch.Tensor,
+                 free_pages: torch.Tensor, n_free: torch.Tensor, lens_out: Optional[torch.Tensor] = None,
+                 n_free_out: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None):
+    """spire_page_release: sequence b is cut to keep[b] tokens, its pages behind go to free_pages."""
+    B, max_blocks = block_table.shape
+    lens_out = lens if lens_out is None else lens_out
+    n_free_out = n_free if n_free_out is None else n_free_out
+    _ints(block_table, lens, keep, free_pages, n_free, lens_out, n_free_out)
+    assert lens.numel() == B and keep.numel() == B and lens_out.numel() == B
+    if ws is None:
+        ws = workspace(page_workspace_size(B), lens.device)
+    _check(load().spire_page_release(block_table.data_ptr(), page_size, max_blocks, lens.data_ptr(),
+                                     keep.data_ptr(), B, free_pages.data_ptr(), free_pages.numel(),
+                                     n_free.data_ptr(), lens_out.data_ptr(), n_free_out.data_ptr(),
+                                     ws.data_ptr(), ws.numel(), _stream()))
+
+
+def rope_view(positions: torch.Tensor, inv_freq: torch.Tensor, axis: Optional[torch.Tensor] = None,
+              interleaved: bool = False) -> Rope:
+    """Describe a rotation as a spire_rope: positions [N] or [axes, N] int32, inv_freq [rot_dim / 2] fp32,
+    axis [rot_dim / 2] int32 (the position axis of each pair) or None for axis 0."""
+    _ints(positions)
+    assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
+    r = Rope()
+    r.positions, r.inv_freq = positions.data_ptr(), inv_freq.data_ptr()
+    if axis is not None:
+        _ints(axis)
+        assert axis.numel() == inv_freq.numel()
+        r.axis = axis.data_ptr()
+    r.axes = positions.shape[0] if positions.dim() == 2 else 1
+    r.rot_dim, r.interleaved, r.reserved = 2 * inv_freq.numel(), int(interleaved), 0
+    r.tokens = positions.shape[-1]  # of this wrapper alone: the calls check it against N
+    r.keep = (positions, inv_freq, axis)
+    return r
+
+
+def _rope(rope: Optional[Rope], N: int):
+    if rope is None:
+        return None
+    assert getattr(rope, "tokens", N) == N, "positions of another number of tokens"
+    return C.byref(rope)
+
+
+def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv: KV, slots: torch.Tensor,
+               rope: Optional[Rope] = None, q_weight: Optional[torch.Tensor] = None,
+               k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+               q_out: Optional[torch.Tensor] = None, out_dtype=None) -> torch.Tensor:
+    """spire_qkv_append.  q [N, Hq, D], k and v [N, Hkv, D] (fp32 or bf16; heads contiguous, any token
+    stride), slots [N] int64, weights [D] fp32; returns q_out [N, Hq, D]."""
+    N, Hq, D = q.shape
+    Hkv = k.shape[1]
+    assert k.shape == (N, Hkv, D) and v.shape == k.shape and q.dtype == k.dtype == v.dtype
+    for t in (q, k, v):
+        assert t.stride(2) == 1 and t.stride(1) == D, "heads must be contiguous"
+    assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == N
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == D)
+    if q_out is None:
+        q_out = torch.empty((N, Hq, D), dtype=out_dtype or q.dtype, device=q.device)
+    assert q_out.shape == q.shape and q_out.is_contiguous()
+    _check(load().spire_qkv_append(q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
+                                   _DT[q.dtype], _ptr(q_weight), _ptr(k_weight), float(eps), _rope(rope, N),
+                                   C.byref(kv), slots.data_ptr(), N, Hq, Hkv, D, q_out.data_ptr(),
+                                   _DT[q_out.dtype], _stream()))
+    return q_out
+
+
+def latent_view(cache: torch.Tensor, Dc: int, block_table: Optional[torch.Tensor] = None,
+                scale: Optional[torch.Tensor] = None, capacity: Optional[int] = None) -> Latent:
+    """Describe 3-d storage [blk, tok, Dc + Dr] (last dimension contiguous) as a spire_latent.  Paged when
+    `block_table` is given (blk = physical page, tok = row of the page), else contiguous (blk = sequence,
+    capacity = size of dim 1 unless given)."""
+    assert cache.dim() == 3 and cache.stride(2) == 1 and 0 < Dc < cache.shape[2]
+    c = Latent()
+    c.c, c.dtype, c.Dc, c.Dr = cache.data_ptr(), _DT[cache.dtype], Dc, cache.shape[2] - Dc
+    c.s_blk, c.s_tok, c.num_blocks = cache.stride(0), cache.stride(1), cache.shape[0]
+    c.scale = _ptr(scale)
+    if block_table is not None:
+        _ints(block_table)
+        c.block_table, c.page_size, c.max_blocks = block_table.data_ptr(), cache.shape[1], block_table.shape[1]
+    else:
+        c.capacity = cache.shape[1] if capacity is None else capacity
+    c.keep = (cache, block_table, scale)
+    return c
+
+
+def latent_append(latent: Latent, c: torch.Tensor, k_rope: torch.Tensor, slots: torch.Tensor,
+                  rope: Optional[Rope] = None, weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                  q_rope: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None):
+    """spire_latent_append.  c [N, Dc], k_rope [N, Dr], q_rope [N, Hq, Dr] (fp32 or bf16, any token and head
+    strides), slots [N] int64, weight [Dc] fp32; q [N, Hq, Dc + Dr] gets the rotated parts in its last Dr."""
+    N, Dc = c.shape
+    assert Dc == latent.Dc and k_rope.shape == (N, latent.Dr) and k_rope.dtype == c.dtype
+    assert c.stride(1) == 1 and k_rope.stride(1) == 1
+    assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == N
+    assert weight is None or (weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == Dc)
+    Hq, qs, qh, qp, op, od = 0, 0, 0, None, None, c.dtype
+    if q_rope is not None:
+        Hq = q_rope.shape[1]
+        assert q_rope.shape == (N, Hq, latent.Dr) and q_rope.dtype == c.dtype and q_rope.stride(2) == 1
+        assert q.shape == (N, Hq, Dc + latent.Dr) and q.is_contiguous()
+        qs, qh, qp, op, od = q_rope.stride(0), q_rope.stride(1), q_rope.data_ptr(), q.data_ptr(), q.dtype
+    _check(load().spire_latent_append(c.data_ptr(), c.stride(0), k_rope.data_ptr(), k_rope.stride(0), qp, qs, qh,
+                                      _DT[c.dtype], _ptr(weight), float(eps), _rope(rope, N), C.byref(latent),
+                                      slots.data_ptr(), N, Hq, op, _DT[od], _stream()))
+
+
+def latent_workspace_size(B, Hq, k, Dc) -> int:
+    return int(load().spire_latent_workspace_size(B, Hq, k, Dc))
+
+
+def latent_verify_attn(q: torch.Tensor, latent: Latent, kv_lens: torch.Tensor, k: int, sm_scale: float,
+                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       ws: Optional[torch.Tensor] = None, out_dtype=torch.float32, with_lse: bool = True,
+                       kernel: int = 0, opts: Optional[LaunchOpts] = None):
+    """spire_latent_verify_attn (the _ex form with a kernel choice or launch events).
+    q [B, k+1, Hq, Dc + Dr]; returns (out [B, k+1, Hq, Dc], lse [B, k+1, Hq])."""
+    B, nq, Hq, Dk = q.shape
+    assert nq == k + 1 and q.is_contiguous() and Dk == latent.Dc + latent.Dr
+    if out is None:
+        out = torch.empty((B, nq, Hq, latent.Dc), dtype=out_dtype, device=q.device)
+    if lse is None and with_lse:
+        lse = torch.empty((B, nq, Hq), dtype=torch.float32, device=q.device)
+    assert out.shape == (B, nq, Hq, latent.Dc) and out.is_contiguous()
+    if ws is None:
+        ws = workspace(latent_workspace_size(B, Hq, k, latent.Dc), q.device)
+    lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)
+    _check(load().spire_latent_verify_attn_ex(q.data_ptr(), _DT[q.dtype], C.byref(latent), lens.data_ptr(), B, Hq, k,
+                                              float(sm_scale), out.data_ptr(), _DT[out.dtype], _ptr(lse),
+                                              ws.data_ptr(), ws.numel(), _stream(), _opts(kernel, opts)))
+    return out, lse
 
 
 def hbm_read_probe(buf: torch.Tensor, sink: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -1,0 +1,242 @@
+"""Norms, rotations and cache writes on the GPU against 64 bits.
+
+Tolerance of an element: half a step of its type (bf16 2^-8, fp8 2^-4 of the value and 2^-10 scales below the normal
+range) plus the fp32 arithmetic before it, 2^-17 of the row's largest element: the sum of squares carries at most
+(D/64 + 8) 2^-24 <= 2^-19 for D <= 1024, root, division and two products four roundings, sine and cosine 2^-21 each
+times at most two elements, and the rotation's own products and sum three roundings."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rope_append as RA
+from paper_2504_06419_amd import spire
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}
+HALF = {"f32": 2.0**-24, "bf16": 2.0**-8, "fp8": 2.0**-4}
+
+
+def close(got, want, kind, scale=1.0):
+    """got in storage values (fp8: codes times scale)."""
+    got = got.double().cpu().numpy() * scale
+    want = np.clip(want, -448 * scale, 448 * scale) if kind == "fp8" else want
+    tol = HALF[kind] * np.abs(want) + 2.0**-17 * np.abs(want).max(-1, keepdims=True)
+    if kind == "fp8":
+        tol = tol + 2.0**-10 * scale
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (kind, np.argwhere(bad)[:3], np.abs(got - want).max())
+
+
+def gen(seed):
+    return torch.Generator(device=DEV).manual_seed(seed)
+
+
+def randn(g, *shape, dt=torch.float32):
+    return torch.randn(*shape, generator=g, device=DEV).to(dt)
+
+
+def same_bits(a, b):
+    return torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8))
+
+
+def run_qkv(N, Hq, Hkv, D, rot, axes=1, inter=False, new="bf16", kv="bf16", ps=16, norm=True, seed=0, out=None,
+            extra=0, shift=0, paged=True, far=1.0, order="hd"):
+    """One call checked whole: queries, written rows, and every other byte of the cache as it was."""
+    g = gen(seed)
+    W = (Hq + 2 * Hkv) * D + extra
+    buf = randn(g, N * W + shift, dt=DT[new])[shift:]
+    proj = buf.view(N, W)
+    x = proj[:, :(Hq + 2 * Hkv) * D].unflatten(1, (Hq + 2 * Hkv, D))
+    q, k, v = x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:]
+    blocks = -(-N // ps) + 2
+    shape = (blocks, Hkv, ps, D) if order == "hd" else (blocks, ps, Hkv, D)
+    kc, vc = ((randn(g, *shape).clamp(-4, 4)).to(DT[kv]) for _ in range(2))
+    if order != "hd":
+        kc, vc = kc.transpose(1, 2), vc.transpose(1, 2)
+    k0, v0 = kc.clone(), vc.clone()
+    slots = torch.randperm(blocks * ps, generator=torch.Generator().manual_seed(seed))[:N]
+    if N > 3:
+        slots[1], slots[2] = -1, blocks * ps  # no storage
+    scale = torch.rand(Hkv, generator=g, device=DEV) * 0.02 + 0.01 if kv == "fp8" else None
+    w1 = randn(g, D) * 0.2 + 1 if norm else None
+    w2 = randn(g, D) * 0.2 + 1 if norm else None
+    pos = (torch.rand(axes, N, generator=g, device=DEV) * 200000 * far).to(torch.int32)
+    pos[:, 0] = 0
+    freq = 1e6 ** (-torch.arange(rot // 2, device=DEV).double() * 2 / max(rot, 1))
+    freq = freq.float()
+    axis = torch.randint(0, axes, (rot // 2,), generator=g, device=DEV, dtype=torch.int32) if axes > 1 else None
+    table = torch.zeros(1, 1, dtype=torch.int32, device=DEV) if paged else None
+    view = spire.kv_view(kc, vc, table, ps if paged else 0, scale, scale)
+    rope = spire.rope_view(pos, freq, axis, inter) if rot else None
+    got = spire.qkv_append(q, k, v, view, slots.to(DEV), rope, w1, w2, 1e-5, out_dtype=DT[out or new])
+    torch.cuda.synchronize()
+    np_ = lambda t: None if t is None else t.double().cpu().numpy()  # noqa: E731
+
+    def through(t, w):
+        return RA.rotate(RA.rms(np_(t), np_(w), 1e-5), np_(pos), np_(freq), None if axis is None else axis.cpu().numpy(), inter)
+
+    close(got, through(q, w1), out or new)
+    ok = (slots >= 0) & (slots < blocks * ps)
+    at = slots[ok]
+    for cache, before, want, sc in ((kc, k0, through(k, w2), scale), (vc, v0, np_(v), scale)):
+        s = 1.0 if sc is None else np_(sc)[None, :, None]
+        close(cache[(at // ps).to(DEV), :, (at % ps).to(DEV)], want[ok.numpy()], kv, s)
+        rest = torch.ones(blocks, ps, dtype=torch.bool)
+        rest[at // ps, at % ps] = False
+        i, j = rest.nonzero(as_tuple=True)
+        bits = lambda t: t.contiguous().view(torch.uint8).view(*t.shape, -1)  # noqa: E731
+        assert torch.equal(bits(cache)[i.to(DEV), :, j.to(DEV)], bits(before)[i.to(DEV), :, j.to(DEV)])
+    return got, kc, vc
+
+
+@pytest.mark.parametrize("N", [1, 2, 5, 64, 333])
+@pytest.mark.parametrize("new,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"),
+                                    ("f32", "fp8")])
+def test_types_and_tokens(N, new, kv):
+    run_qkv(N, 8, 2, 128, 128, new=new, kv=kv, seed=N)
+
+
+@pytest.mark.parametrize("D,rot", [(64, 64), (128, 64), (256, 256), (256, 64), (128, 0), (96, 96), (80, 40), (112, 112), (72, 8),
+                                   (7, 6), (1, 0), (130, 130), (100, 50), (1024, 1024), (512, 128), (192, 64)])
+@pytest.mark.parametrize("inter", [False, True])
+@pytest.mark.parametrize("new", ["bf16", "f32"])
+def test_head_sizes(D, rot, inter, new):
+    run_qkv(9, 3, 2, D, rot, inter=inter, new=new, kv=new, seed=D + rot)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (64, 8), (5, 5), (20, 4), (128, 1), (7, 1)])
+@pytest.mark.parametrize("axes,inter", [(1, False), (2, True), (3, False), (4, True)])
+def test_heads_and_axes(Hq, Hkv, axes, inter):
+    run_qkv(17, Hq, Hkv, 128, 128, axes, inter, seed=Hq + axes)
+
+
+@pytest.mark.parametrize("kw", [dict(norm=False), dict(extra=8), dict(extra=3), dict(shift=1), dict(shift=4), dict(shift=8),
+                                dict(paged=False), dict(ps=1), dict(ps=7), dict(ps=256), dict(out="f32"),
+                                dict(new="f32", out="bf16", kv="f32"), dict(far=10000.0), dict(order="th"),
+                                dict(norm=False, rot=0), dict(new="f32", shift=1), dict(new="f32", kv="f32", extra=2)])
+def test_layouts(kw):
+    kw = dict(dict(rot=128), **kw)
+    run_qkv(21, 8, 2, 128, seed=3, **kw)
+
+
+def test_the_sum_of_zeros():
+    """A row of zeros with eps = 0 is 0/0 by definition, with eps > 0 it is zero."""
+    q = torch.zeros(2, 1, 64, device=DEV)
+    c = torch.ones(1, 1, 4, 64, device=DEV)
+    d, table = c.clone(), torch.zeros(1, 1, dtype=torch.int32, device=DEV)  # a view keeps no tensor alive
+    view = spire.kv_view(c, d, table, 4)
+    w = torch.ones(64, device=DEV)
+    slots = torch.tensor([0, 1], device=DEV)
+    assert torch.all(spire.qkv_append(q, q, q, view, slots, None, w, w, 1e-6) == 0)
+    assert torch.all(torch.isnan(spire.qkv_append(q, q, q, view, slots, None, w, w, 0.0)))
+
+
+def test_axis_values_are_clamped():
+    g = gen(1)
+    N, D = 4, 64
+    q, f = randn(g, N, 2, D), torch.rand(D // 2, generator=g, device=DEV)
+    c = torch.zeros(1, 2, 4, D, device=DEV)
+    d, table = c.clone(), torch.zeros(1, 1, dtype=torch.int32, device=DEV)  # a view keeps no tensor alive
+    view = spire.kv_view(c, d, table, 4)
+    pos = torch.randint(0, 50, (2, N), generator=g, device=DEV, dtype=torch.int32)
+    axis = torch.full((D // 2,), 77, dtype=torch.int32, device=DEV)
+    axis[:5] = -3
+    got = spire.qkv_append(q, q, q, view, torch.arange(N, device=DEV), spire.rope_view(pos, f, axis))
+    want = RA.rotate(q.double().cpu().numpy(), pos.cpu().numpy(), f.cpu().numpy(), axis.cpu().numpy())
+    close(got, want, "f32")
+
+
+def run_latent(N, Hq, Dc, Dr, inter=True, new="bf16", kv="bf16", ps=16, norm=True, seed=0, extra=0, shift=0, queries=True,
+               out=None, tok=0):
+    g = gen(seed)
+    proj = randn(g, N * (Dc + Dr + extra) + shift, dt=DT[new])[shift:].view(N, Dc + Dr + extra)
+    qp = randn(g, N, Hq, 40 + Dr, dt=DT[new])
+    blocks = -(-N // ps) + 2
+    whole = randn(g, blocks, ps, Dc + Dr + tok).clamp(-4, 4).to(DT[kv])
+    cache = whole[..., :Dc + Dr]
+    before = whole.clone()
+    slots = torch.randperm(blocks * ps, generator=torch.Generator().manual_seed(seed))[:N]
+    if N > 3:
+        slots[0], slots[3] = -5, 2**40
+    scale = torch.full((1,), 0.015, device=DEV) if kv == "fp8" else None
+    w = randn(g, Dc) * 0.2 + 1 if norm else None
+    pos = torch.randint(0, 131072, (1, N), generator=g, device=DEV, dtype=torch.int32)
+    freq = (1e4 ** (-torch.arange(Dr // 2, device=DEV).double() * 2 / Dr)).float()
+    q = torch.full((N, Hq, Dc + Dr), 3.0, device=DEV, dtype=DT[out or new])
+    rope = spire.rope_view(pos, freq, interleaved=inter)
+    spire.latent_append(spire.latent_view(cache, Dc, scale=scale), proj[:, :Dc], proj[:, Dc:Dc + Dr], slots.to(DEV), rope, w, 1e-6,
+                        q_rope=qp[..., 40:] if queries else None, q=q if queries else None)
+    torch.cuda.synchronize()
+    np_ = lambda t: t.double().cpu().numpy()  # noqa: E731
+    turn = lambda t: RA.rotate(np_(t), np_(pos), np_(freq), None, inter)  # noqa: E731
+    assert torch.all(q[..., :Dc] == 3)
+    if queries:
+        close(q[..., Dc:], turn(qp[..., 40:]), out or new)
+    else:
+        assert torch.all(q == 3)
+    ok = (slots >= 0) & (slots < blocks * ps)
+    at = slots[ok].to(DEV)
+    s = 1.0 if scale is None else 0.015
+    lat = RA.rms(np_(proj[:, :Dc]), None if w is None else np_(w), 1e-6)
+    got = cache[at // ps, at % ps]
+    close(got[:, :Dc], lat[ok.numpy()], kv, s)
+    close(got[:, Dc:], turn(proj[:, None, Dc:Dc + Dr])[:, 0][ok.numpy()], kv, s)
+    bits = lambda t: t.contiguous().view(torch.uint8).view(blocks * ps, -1)  # noqa: E731
+    a, b = bits(whole).clone(), bits(before)
+    row = (Dc + Dr) * whole.element_size()
+    a[at, :row] = b[at, :row]
+    assert torch.equal(a, b)  # rows of other tokens and what lies between rows
+
+
+@pytest.mark.parametrize("N", [1, 3, 64, 333])
+@pytest.mark.parametrize("new,kv", [("bf16", "bf16"), ("bf16", "fp8"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("f32", "fp8")])
+def test_latent_types_and_tokens(N, new, kv):
+    run_latent(N, 16, 512, 64, new=new, kv=kv, seed=N)
+
+
+@pytest.mark.parametrize("Dc,Dr", [(256, 64), (512, 32), (128, 64), (384, 64), (100, 6), (7, 2), (1024, 128), (515, 66), (4096, 64)])
+@pytest.mark.parametrize("inter", [False, True])
+def test_latent_sizes(Dc, Dr, inter):
+    run_latent(9, 5, Dc, Dr, inter, seed=Dc)
+
+
+@pytest.mark.parametrize("kw", [dict(norm=False), dict(extra=8), dict(extra=3), dict(shift=1), dict(shift=8), dict(ps=1), dict(ps=7),
+                                dict(queries=False), dict(out="f32"), dict(tok=8), dict(tok=3), dict(Hq=1), dict(Hq=128), dict(Hq=20),
+                                dict(inter=False), dict(new="f32", shift=1, kv="f32"), dict(kv="fp8", tok=5)])
+def test_latent_layouts(kw):
+    run_latent(**dict(dict(N=13, Hq=16, Dc=512, Dr=64, seed=5), **kw))
+
+
+def test_in_a_graph_and_on_another_stream():
+    g = gen(8)
+    N, Hq, Hkv, D = 40, 8, 2, 128
+    x = randn(g, N, Hq + 2 * Hkv, D, dt=torch.bfloat16)
+    kc = torch.zeros(4, Hkv, 16, D, device=DEV, dtype=torch.bfloat16)
+    vc = torch.zeros_like(kc)
+    view = spire.kv_view(kc, vc, torch.zeros(1, 1, dtype=torch.int32, device=DEV), 16)
+    pos, f = torch.arange(N, device=DEV, dtype=torch.int32), torch.rand(D // 2, generator=g, device=DEV)
+    slots, out = torch.arange(N, device=DEV), torch.empty(N, Hq, D, device=DEV, dtype=torch.bfloat16)
+    rope, w = spire.rope_view(pos, f), torch.ones(D, device=DEV)
+
+    def call():
+        spire.qkv_append(x[:, :Hq], x[:, Hq:Hq + Hkv], x[:, Hq + Hkv:], view, slots, rope, w, w, q_out=out)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(4):
+        x.copy_(randn(g, N, Hq + 2 * Hkv, D))
+        pos.add_(1000)
+        kc.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        a = [t.clone() for t in (out, kc, vc)]
+        call()
+        torch.cuda.synchronize()
+        assert all(same_bits(p, q) for p, q in zip(a, (out, kc, vc))) and kc.abs().sum() > 0
