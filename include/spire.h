@@ -504,7 +504,7 @@ spire_status spire_latent_append(const void *c_new, int64_t c_stride, const void
 
 /* Bytes of workspace spire_latent_verify_attn needs for these sizes on the
  * current device (0 on invalid sizes). */
-size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc);
+size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc, int32_t Dr);
 
 /*
  * Target verification attention over a latent cache, absorbed form: the
@@ -518,7 +518,7 @@ size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc)
  *            SPIRE_F32 or SPIRE_BF16; lse [B, k+1, Hq] fp32 natural log, or NULL.
  *   sizes    0 <= B <= 8192, 1 <= Hq <= 128, 0 <= k <= 15, Dc 256 or 512, Dr = 64
  *            (SPIRE_ERR_UNSUPPORTED otherwise).
- *   workspace >= spire_latent_workspace_size(B, Hq, k, Dc) bytes, 256-byte aligned.
+ *   workspace >= spire_latent_workspace_size(B, Hq, k, Dc, Dr) bytes, 256-byte aligned.
  * bf16 queries on bf16 or fp8 caches whose rows start 16-byte aligned run on the
  * 16-bit matrix instructions (probabilities rounded to 16 bits, sums in fp32),
  * everything else in fp32.  Non-finite values act as for spire_verify_attn;

@@ -1033,8 +1033,9 @@ static Layout latent_layout(int B, int Dc, const LatentShape &s) {
     return layout(B, (int64_t)s.units * s.nb * 16, Dc, s.groups);
 }
 
-size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc) {
-    if (B < 0 || B > kPlanMaxB || Hq < 1 || Hq > 128 || k < 0 || k > 15 || (Dc != 256 && Dc != 512)) return 0;
+size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc, int32_t Dr) {
+    if (B < 0 || B > kPlanMaxB || Hq < 1 || Hq > 128 || k < 0 || k > 15 || (Dc != 256 && Dc != 512) || Dr != kLatentDr)
+        return 0;
     int cus = 0;
     if (device_cus(&cus) != 0) return 0;
     return latent_layout(B, Dc, latent_shape(Hq, k, cus)).total;

@@ -150,7 +150,7 @@ def load(path: Optional[str] = None):
     L.spire_latent_append.argtypes = [vp, i64, vp, i64, vp, i64, i64, i32, vp, f32, C.POINTER(Rope),
                                       C.POINTER(Latent), vp, i32, i32, vp, i32, vp]
     L.spire_latent_workspace_size.restype = sz
-    L.spire_latent_workspace_size.argtypes = [i32] * 4
+    L.spire_latent_workspace_size.argtypes = [i32] * 5
     L.spire_latent_verify_attn.restype = C.c_int
     L.spire_latent_verify_attn.argtypes = [vp, i32, C.POINTER(Latent), vp, i32, i32, i32, f32, vp, i32, vp, vp, sz, vp]
     L.spire_latent_verify_attn_ex.restype = C.c_int
@@ -572,8 +572,8 @@ def latent_append(latent: Latent, c: torch.Tensor, k_rope: torch.Tensor, slots: 
                                       slots.data_ptr(), N, Hq, op, _DT[od], _stream()))
 
 
-def latent_workspace_size(B, Hq, k, Dc) -> int:
-    return int(load().spire_latent_workspace_size(B, Hq, k, Dc))
+def latent_workspace_size(B, Hq, k, Dc, Dr) -> int:
+    return int(load().spire_latent_workspace_size(B, Hq, k, Dc, Dr))
 
 
 def latent_verify_attn(q: torch.Tensor, latent: Latent, kv_lens: torch.Tensor, k: int, sm_scale: float,
@@ -590,7 +590,7 @@ def latent_verify_attn(q: torch.Tensor, latent: Latent, kv_lens: torch.Tensor, k
         lse = torch.empty((B, nq, Hq), dtype=torch.float32, device=q.device)
     assert out.shape == (B, nq, Hq, latent.Dc) and out.is_contiguous()
     if ws is None:
-        ws = workspace(latent_workspace_size(B, Hq, k, latent.Dc), q.device)
+        ws = workspace(latent_workspace_size(B, Hq, k, latent.Dc, latent.Dr), q.device)
     lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)
     _check(load().spire_latent_verify_attn_ex(q.data_ptr(), _DT[q.dtype], C.byref(latent), lens.data_ptr(), B, Hq, k,
                                               float(sm_scale), out.data_ptr(), _DT[out.dtype], _ptr(lse),

@@ -243,7 +243,7 @@ def test_streams_workspaces_and_graphs():
     eager calls between; the workspace's content does not matter."""
     inps = [Inp([3000, 17, 900], 16, 4, ps=64, seed=s) for s in (31, 32)]
     want = [i.run() for i in inps]
-    wss = [spire.workspace(spire.latent_workspace_size(3, 16, 4, 512)).fill_(255) for _ in inps]
+    wss = [spire.workspace(spire.latent_workspace_size(3, 16, 4, 512, 64)).fill_(255) for _ in inps]
     streams, got = [torch.cuda.Stream() for _ in inps], []
     torch.cuda.synchronize()
     for _ in range(3):

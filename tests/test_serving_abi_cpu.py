@@ -172,7 +172,8 @@ def test_latent_attention_refusals(kw, status):
 
 def test_workspace_of_invalid_sizes():
     L = spire.load()
-    for a in [(-1, 16, 0, 512), (1, 0, 0, 512), (1, 129, 0, 512), (1, 16, 16, 512), (1, 16, 0, 128), (9000, 16, 0, 512)]:
+    for a in [(-1, 16, 0, 512, 64), (1, 0, 0, 512, 64), (1, 129, 0, 512, 64), (1, 16, 16, 512, 64), (1, 16, 0, 128, 64),
+              (9000, 16, 0, 512, 64), (1, 16, 0, 512, 32)]:
         assert L.spire_latent_workspace_size(*a) == 0
     assert L.spire_page_workspace_size(-1) == 0 and L.spire_page_workspace_size(8193) == 0
     assert L.spire_page_workspace_size(0) > 0
