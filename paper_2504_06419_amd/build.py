@@ -19,7 +19,8 @@ ARCH = "gfx950"
 
 SOURCES = ["spire_abi.hip", "plan_combine.hip", "attn_mfma.hip", "attn_staged.hip",
            "attn_generic.hip", "attn_f32.hip", "token_verify.hip", "block_verify.hip", "kv_update.hip",
-           "feedback_memory.hip", "hbm_probe.hip", "pages.hip", "rope_append.hip", "latent_attn.hip"]
+           "feedback_memory.hip", "hbm_probe.hip", "pages.hip", "rope_append.hip", "latent_attn.hip",
+           "latent_mfma.hip"]
 
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -32,7 +33,7 @@ FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
 # rarely taken rescale branch into every tile.
 MFMA_FLAGS = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 SOURCE_FLAGS = {"attn_mfma.hip": MFMA_FLAGS, "attn_staged.hip": MFMA_FLAGS, "attn_f32.hip": MFMA_FLAGS,
-                "latent_attn.hip": MFMA_FLAGS}
+                "latent_attn.hip": MFMA_FLAGS, "latent_mfma.hip": MFMA_FLAGS}
 
 
 def _hipcc():

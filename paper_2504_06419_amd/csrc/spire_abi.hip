@@ -1020,11 +1020,13 @@ spire_status spire_latent_append(const void *c_new, int64_t c_stride, const void
 // Blocks per unit and groups of a launch (latent_common.h).
 struct LatentShape { int nb, units, groups; };
 
-static LatentShape latent_shape(int Hq, int k, int cus) {
-    const int blocks = (k + 1) * ((Hq + 15) / 16);
+// The matrix kernel holds up to 4 blocks, evenly spread over the units (5 blocks:
+// 3 + 2), the fp32 kernel one.
+static LatentShape latent_shape(int Hq, int k, int cus, bool matrix) {
+    const int blocks = (k + 1) * ((Hq + 15) / 16), most = matrix ? 4 : 1;
     LatentShape s;
-    s.nb = 1;
-    s.units = blocks;
+    s.units = (blocks + most - 1) / most;
+    s.nb = (blocks + s.units - 1) / s.units;
     s.groups = std::max(1, cus / s.units);
     return s;
 }
@@ -1038,7 +1040,8 @@ size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc,
         return 0;
     int cus = 0;
     if (device_cus(&cus) != 0) return 0;
-    return latent_layout(B, Dc, latent_shape(Hq, k, cus)).total;
+    return std::max(latent_layout(B, Dc, latent_shape(Hq, k, cus, false)).total,
+                    latent_layout(B, Dc, latent_shape(Hq, k, cus, true)).total);
 }
 
 spire_status spire_latent_verify_attn(const void *q, int32_t q_dtype, const spire_latent *latent,
@@ -1104,18 +1107,23 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
     p.out = out;
     p.out_dtype = out_dtype;
     p.lse = lse;
-    const LatentShape sh = latent_shape(Hq, k, cus);
+    const int es = p.kv.elem;
+    // matrix kernel: 16-byte copies, 16 rows within 32-bit lane offsets
+    const bool matrix = q_dtype == SPIRE_BF16 && latent->dtype != SPIRE_F32 && !(opts != nullptr && opts->kernel == 1) &&
+                        aligned16(latent->c) && (latent->s_blk * es) % 16 == 0 && (latent->s_tok * es) % 16 == 0 &&
+                        (uint64_t)latent->s_tok * es * 16 < (1ull << 31);
+    const LatentShape sh = latent_shape(Hq, k, cus, matrix);
     a.hb = (Hq + 15) / 16;
     a.nb = sh.nb;
     a.units = sh.units;
-    const int es = p.kv.elem;
+    a.uniform = latent->page_size % 16 == 0;
     a.quads = (uintptr_t)latent->c % (4 * es) == 0 && latent->s_blk % 4 == 0 && latent->s_tok % 4 == 0;
     Plan &pl = a.pl;
-    pl.tile = 32;
+    pl.tile = matrix ? 64 : 32;
     pl.units = 1;
     pl.rows = sh.units * sh.nb * 16;
     pl.workers = sh.groups;
-    pl.seg_cost = 0;
+    pl.seg_cost = matrix ? 2 : 0;
     const Layout L = latent_layout(B, p.D, sh);
     if (workspace_bytes < L.total)
         return fail(SPIRE_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, L.total);
@@ -1128,7 +1136,7 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
     Recorder rec(opts);
     hipError_t e = rec.run(KID_PLAN, stream, launch_plan, p, pl);
     if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "plan launch: %s", hipGetErrorString(e));
-    e = rec.run(KID_LATENT, stream, [&] { return launch_latent_f32(a, stream); });
+    e = rec.run(KID_LATENT, stream, [&] { return matrix ? launch_latent_mfma(a, stream) : launch_latent_f32(a, stream); });
     if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "latent attention launch: %s", hipGetErrorString(e));
     e = rec.run(KID_LATENT_COMBINE, stream, [&] { return launch_latent_combine(a, stream); });
     if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "latent combine launch: %s", hipGetErrorString(e));
