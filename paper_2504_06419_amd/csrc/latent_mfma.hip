@@ -54,6 +54,21 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 
 constexpr int kLatTile = 64;
 
+// whether one of 8 bf16 (16 e4m3fn) values is not finite
+template <bool FP8> __device__ __forceinline__ bool any_nonfinite(u32x4 v) {
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (FP8) {
+#pragma unroll
+            for (int s = 0; s < 32; s += 8) bad |= ((v[i] >> s) & 0x7Fu) == 0x7Fu;
+        } else {
+            bad |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
+        }
+    }
+    return bad;
+}
+
 // Keeps a lane's address a value of the current tile: what is derived from it (an
 // exclusive-or per read) is formed where it is used.  Hoisted out of the tile loop
 // the derived addresses would take some 50 registers.
@@ -355,15 +370,24 @@ const uint32_t ln = here(lane);
                         }
                     }
                 };
+                // A hidden key's probability is 0, which clears any finite value; what is not
+                // finite in this wave's 16 rows from the first hidden key on is looked for.
+                bool bad = false;
+                if (tail) {
+                    for (int i = lane; i < 16 * G::CH; i += 64)
+                        if (key0 + 16 * wave + i / G::CH >= least)
+                            bad |= any_nonfinite<FP8>(lds_read<u32x4>(st + wave * 16 * G::RB + 16 * i));
+                }
                 bool over = false;
 #pragma unroll
                 for (int x = 0; x < NW; ++x) over |= top(x) > thr[x];
-                const bool any = __any(over);
+                const int word = (__any(over) ? 1 : 0) | (__any(bad) ? 2 : 0);
                 weigh();
-                if (lane == 0) flags[wave] = any;
+                if (lane == 0) flags[wave] = word;
                 lds_barrier();
                 const int4 fl = *reinterpret_cast<const int4 *>(flags);
-                if (__builtin_amdgcn_readfirstlane(fl.x | fl.y | fl.z | fl.w)) {
+                const int events = __builtin_amdgcn_readfirstlane(fl.x | fl.y | fl.z | fl.w);
+                if (events & 1) {
                     // some row's scores pass its reference: move the references of all waves
 #pragma unroll
                     for (int x = 0; x < NW; ++x) {
@@ -410,6 +434,42 @@ const uint32_t ln = here(lane);
 #pragma unroll
                 for (int x = 0; x < NW; ++x) l[x] += add[x];
 
+                if (events & 2) {
+                    // A value that is not finite makes its dimension NaN in the rows that see its
+                    // key (the key's score is not finite either); then it is cleared.
+                    const int stop = n < key0 + kLatTile ? n : key0 + kLatTile;
+                    for (int key = least > key0 ? least : key0; key < stop; ++key) {
+                        const int r = key - key0;
+#pragma unroll
+                        for (int y = 0; y < XB; ++y) {
+                            const int d = wave * (DC / 4) + 16 * y + 4 * j, byte = d * G::ES;
+                            const uint32_t at = st + r * G::RB + 16 * ((byte >> 4) ^ fm(r & 15)) + (byte & 15);
+                            f32x4 nan;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const bool not_finite = FP8 ? (lds_read<uint8_t>(at + e) & 0x7F) == 0x7F
+                                                            : (lds_read<uint16_t>(at + 2 * e) & 0x7F80) == 0x7F80;
+                                nan[e] = not_finite ? __builtin_nanf("") : 0.f;
+                            }
+#pragma unroll
+                            for (int x = 0; x < NB; ++x)
+                                if (key < limit(x)) acc[y][x] += nan;
+                        }
+                    }
+                    lds_barrier();
+                    for (int i = lane; i < 16 * G::CH; i += 64)
+                        if (key0 + 16 * wave + i / G::CH >= least) {
+                            const uint32_t at = st + wave * 16 * G::RB + 16 * i;
+                            if (any_nonfinite<FP8>(lds_read<u32x4>(at)))
+                                for (int e = 0; e < 16; e += G::ES)
+                                    if (FP8 ? (lds_read<uint8_t>(at + e) & 0x7F) == 0x7F : (lds_read<uint16_t>(at + e) & 0x7F80) == 0x7F80) {
+                                        if constexpr (FP8) *reinterpret_cast<__attribute__((address_space(3))) uint8_t *>((lds_u8 *)(uintptr_t)(at + e)) = 0;
+                                        else *reinterpret_cast<__attribute__((address_space(3))) uint16_t *>((lds_u8 *)(uintptr_t)(at + e)) = 0;
+                                    }
+                        }
+                    lds_barrier();
+                }
+
                 // ---- O^T += C^T P^T ----------------------------------------------
                 // C^T operand of output block y and keys 32 ks .. + 31
                 const uint32_t vat = here(st + v0);
@@ -433,50 +493,30 @@ const uint32_t ln = here(lane);
                     if constexpr (FP8) return fp8x8_to_f16x8(r.x, r.y);
                     else return r;
                 };
-                if (!tail) {
-                    constexpr int VG = 4;  // operands a group ahead
-                    decltype(read_v(0)) vb[2][VG];
-                    u32x4 pf[NB];
+                constexpr int VG = 4;  // operands a group ahead
+                decltype(read_v(0)) vb[2][VG];
+                u32x4 pf[NB];
 #pragma unroll
-                    for (int x = 0; x < NB; ++x) pf[x] = lds_read<u32x4>(pread0 + 2048 * x);
+                for (int x = 0; x < NB; ++x) pf[x] = lds_read<u32x4>(pread0 + 2048 * x);
 #pragma unroll
-                    for (int y = 0; y < VG; ++y) vb[0][y] = read_v(y);
+                for (int y = 0; y < VG; ++y) vb[0][y] = read_v(y);
 #pragma unroll
-                    for (int i0 = 0; i0 < 2 * XB; i0 += VG) {
-                        const int cur = (i0 / VG) & 1;
-                        if (i0 == XB) {
+                for (int i0 = 0; i0 < 2 * XB; i0 += VG) {
+                    const int cur = (i0 / VG) & 1;
+                    if (i0 == XB) {
 #pragma unroll
-                            for (int x = 0; x < NB; ++x) pf[x] = lds_read<u32x4>((pread0 ^ 64) + 2048 * x);
-                        }
-#pragma unroll
-                        for (int y = 0; y < VG; ++y)
-                            if (i0 + VG + y < 2 * XB) vb[cur ^ 1][y] = read_v(i0 + VG + y);
-#pragma unroll
-                        for (int y = 0; y < VG; ++y) {
-                            const u32x4 v = value(vb[cur][y]);
-#pragma unroll
-                            for (int x = 0; x < NB; ++x) acc[(i0 + y) % XB][x] = mfma_pv<FP8>(v, pf[x], acc[(i0 + y) % XB][x]);
-                        }
-                        __builtin_amdgcn_sched_barrier(0);
+                        for (int x = 0; x < NB; ++x) pf[x] = lds_read<u32x4>((pread0 ^ 64) + 2048 * x);
                     }
-                } else {
-                    // keys hidden from a block are zero in its operands, whatever they hold
 #pragma unroll
-                    for (int x = 0; x < NB; ++x)
+                    for (int y = 0; y < VG; ++y)
+                        if (i0 + VG + y < 2 * XB) vb[cur ^ 1][y] = read_v(i0 + VG + y);
 #pragma unroll
-                        for (int ks = 0; ks < 2; ++ks) {
-                            const int seen = limit(x);
-                            u32x4 mask;
+                    for (int y = 0; y < VG; ++y) {
+                        const u32x4 v = value(vb[cur][y]);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const int key = key0 + 32 * ks + 8 * j + 2 * e;
-                                mask[e] = (key < seen ? 0xFFFFu : 0u) | (key + 1 < seen ? 0xFFFF0000u : 0u);
-                            }
-                            const u32x4 pf = lds_read<u32x4>((pread0 ^ (64 * ks)) + 2048 * x);
-#pragma unroll
-                            for (int y = 0; y < XB; ++y) acc[y][x] = mfma_pv<FP8>(value(read_v(ks * XB + y)) & mask, pf, acc[y][x]);
-                            __builtin_amdgcn_sched_barrier(0);
-                        }
+                        for (int x = 0; x < NB; ++x) acc[(i0 + y) % XB][x] = mfma_pv<FP8>(v, pf[x], acc[(i0 + y) % XB][x]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
             wait_vmcnt<0>();  // no copy is still landing when the ring is used again
