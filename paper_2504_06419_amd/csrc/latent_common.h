@@ -18,9 +18,6 @@
 
 namespace spire {
 
-// Matrix kernel: waves that share the rows of a unit's scores (latent_mfma.hip).
-constexpr int latent_row_split(int Dc, int nb) { return Dc == 512 && nb == 4 ? 2 : 1; }
-
 // Workgroup -> (group, unit).  Workgroups that follow each other go to different
 // XCDs (blockIdx % 8), each with an L2 of its own; neighbours in `lin` share one,
 // so a group's workgroups read their common keys through one L2.

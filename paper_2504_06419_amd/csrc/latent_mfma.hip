@@ -80,6 +80,14 @@ __device__ __forceinline__ uint32_t here_s(uint32_t x) {
     asm volatile("" : "+s"(x));
     return x;
 }
+// The kernel's arguments, read again from where it is called: what is used once per
+// segment does not occupy scalar registers through the tile loop.
+typedef const Latent __attribute__((address_space(4))) cLatent;
+__device__ __forceinline__ cLatent *arguments() {
+    uint64_t x = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(x));
+    return (cLatent *)x;
+}
 template <class V> __device__ __forceinline__ V lds_read(uint32_t at) {
     return *reinterpret_cast<const __attribute__((address_space(3))) V *>((const lds_u8 *)(uintptr_t)at);
 }
@@ -87,40 +95,44 @@ template <class V> __device__ __forceinline__ V lds_read(uint32_t at) {
 // Stage of one tile: [64][DC] rows, then [64][64] rotated parts.  16-byte chunk q of
 // row r lies at q ^ fm(r) (main part, low 4 bits) and q ^ fr(r): operand reads (16
 // rows, one chunk) and transposing reads (4 rows, 2 chunks) hit distinct banks.
-template <int DC, bool FP8> struct LatStage {
+template <int DC, bool FP8, int WAVES> struct LatStage {
     static constexpr int ES = FP8 ? 1 : 2;
     static constexpr int RB = DC * ES, RR = kLatentDr * ES;  // bytes of a row's parts
     static constexpr int MAIN = kLatTile * RB;
     static constexpr int BYTES = kLatTile * (RB + RR);
     static constexpr int CH = RB / 16, RCH = RR / 16;        // chunks of a row's parts
-    static constexpr int ML = 16 * CH / 64, RL = 16 * RCH / 64;  // copies of a wave's 16 rows
+    static constexpr int ROWS = kLatTile / WAVES;            // rows a wave copies
+    static constexpr int ML = ROWS * CH / 64, RL = (ROWS * RCH + 63) / 64;  // its copies
     static constexpr int LOADS = ML + RL;
 };
 __device__ __forceinline__ int fm(int r) { return ((r & 7) << 1) | ((r >> 3) & 1); }
 template <bool FP8> __device__ __forceinline__ int fr(int r) { return FP8 ? (r >> 2) & 3 : (r >> 1) & 7; }
 
-template <int DC, bool FP8, int NB>
-__global__ __launch_bounds__(256, 1) void latent_mfma_kernel(Latent a) {
-    using G = LatStage<DC, FP8>;
+template <int DC, bool FP8, int NB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES / 4) void latent_mfma_kernel(Latent a) {
+    using G = LatStage<DC, FP8, WAVES>;
     constexpr int DK = DC + kLatentDr;
     constexpr int STEPS = DK / 32;      // QK steps of 32 dimensions
-    constexpr int XB = DC / 64;         // 16-dimension output blocks of a wave
-    constexpr int RW = latent_row_split(DC, NB), KW = 4 / RW;  // scores: waves along rows, along keys
-    constexpr int NW = NB / RW, KB = 4 / KW;                   // a wave's row blocks and 16-key blocks
+    constexpr int XB = DC / (16 * WAVES);                // 16-dimension output blocks of a wave
+    constexpr int KW = 4, RW = WAVES / KW, NW = NB / RW;  // scores: waves along keys, along rows; a wave's row blocks
     static_assert(NB % RW == 0, "row blocks split evenly");
     constexpr int PB = NB * 16 * 128;   // P: [rows][64 keys] 16-bit
-    constexpr int NS0 = (160 * 1024 - PB - 2048) / G::BYTES, NS = NS0 > 4 ? 4 : NS0;
+    // Two waves per SIMD have 256 registers each: with 4 blocks of a 512-wide latent the
+    // last QL steps of the queries stay in LDS (fp8 stages are half as large: one less).
+    constexpr int QL = DC == 512 && NB == 4 ? (FP8 ? 4 : 1) : 0, QR = STEPS - QL;
+    constexpr int QBYTES = QL * NB * 1024;
+    constexpr int NS0 = (160 * 1024 - PB - QBYTES - 2048) / G::BYTES, NS = NS0 > 4 ? 4 : NS0;
     static_assert(NS >= 2, "stage ring too small");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * G::BYTES + PB + (KW + 1) * NB * 64 + 16];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * G::BYTES + QBYTES + PB + (KW + 1) * NB * 64 + 4 * WAVES];
     lds_u8 *ring = (lds_u8 *)smem;
-    lds_u8 *pbuf = ring + NS * G::BYTES;
-    float *red = reinterpret_cast<float *>(smem + NS * G::BYTES + PB);  // [KW][16 NB]
+    lds_u8 *pbuf = ring + NS * G::BYTES + QBYTES;
+    float *red = reinterpret_cast<float *>(smem + NS * G::BYTES + QBYTES + PB);  // [KW][16 NB]
     float *refs = red + KW * 16 * NB;                                  // [16 NB] references, -inf: none yet
-    int *flags = reinterpret_cast<int *>(refs + 16 * NB);              // [4]
+    int *flags = reinterpret_cast<int *>(refs + 16 * NB);              // [WAVES]
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int kw = RW == 1 ? wave : wave & (KW - 1), rw = RW == 1 ? 0 : wave / KW;
+    const int kw = wave & (KW - 1), rw = wave / KW;
     const int n16 = lane & 15, j = lane >> 4;
     const Problem &p = a.p;
     const Plan &pl = a.pl;
@@ -143,15 +155,16 @@ __global__ __launch_bounds__(256, 1) void latent_mfma_kernel(Latent a) {
     // lane constants of the LDS reads
     // (chunk 4 c + j of a row at 16 ((4 c + j) ^ f): only bits 4-7 of the address change with c & 3)
     const uint32_t ring0 = (uint32_t)(uintptr_t)ring;
-    const uint32_t kmain0 = (uint32_t)(16 * KB * kw + n16) * G::RB + 16 * (j ^ fm(n16));
-    const uint32_t krope0 = (uint32_t)G::MAIN + (uint32_t)(16 * KB * kw + n16) * G::RR + 16 * (j ^ fr<FP8>(n16));
+    const uint32_t kmain0 = (uint32_t)(16 * kw + n16) * G::RB + 16 * (j ^ fm(n16));
+    const uint32_t krope0 = (uint32_t)G::MAIN + (uint32_t)(16 * kw + n16) * G::RR + 16 * (j ^ fr<FP8>(n16));
     // transposing reads: bf16: lane s of group j addresses key 8 j + 4 h + s / 4, 4 dimensions, and receives
     // dimension s of the group's 4 keys; fp8: key 8 j + s / 2, 8 dimensions, and receives dimension s of 8 keys
     const int vr = FP8 ? 8 * j + (n16 >> 1) : 8 * j + (n16 >> 2);
     const uint32_t v0 = (uint32_t)vr * G::RB + 16 * ((FP8 ? XB * wave : 2 * XB * wave + ((n16 >> 1) & 1)) ^ fm(vr & 15)) + 8 * (n16 & 1);
+    const uint32_t q0 = ring0 + NS * G::BYTES + 1024 * NW * rw + 16 * lane;  // queries in LDS: [QL][NB][64 lanes]
     const uint32_t p0 = (uint32_t)(uintptr_t)pbuf + n16 * 128;
     const uint32_t pread0 = p0 + 16 * (j ^ (n16 & 7));
-    const uint32_t pwrite0 = p0 + 2048 * NW * rw + 16 * ((2 * KB * kw + (j >> 1)) ^ (n16 & 7)) + 8 * (j & 1);
+    const uint32_t pwrite0 = p0 + 2048 * NW * rw + 16 * ((2 * kw + (j >> 1)) ^ (n16 & 7)) + 8 * (j & 1);
     const uint32_t tok_bytes = (uint32_t)(p.kv.s_tok * G::ES);
 
     while (pos < end) {
@@ -170,18 +183,20 @@ __global__ __launch_bounds__(256, 1) void latent_mfma_kernel(Latent a) {
         const int n = uload(pl.nkeys, b);
         // keys that block x of the unit sees; the first block sees the fewest
         auto limit = [&](int x) {
-            const int i = (u * NB + x) / a.hb;
-            return n - p.k + (i <= p.k ? i : p.k);
+            cLatent *A = arguments();
+            const int i = (u * NB + x) / A->hb, k = A->p.k;
+            return n - k + (i <= k ? i : k);
         };
         const int least = limit(0);
         int lim[NW];
 #pragma unroll
         for (int x = 0; x < NW; ++x) lim[x] = limit(NW * rw + x);
         // query of this lane in block x, or a neighbour's where the block has fewer rows
-        auto row_of = [&](int x, bool &ok) {
-            const int rb = u * NB + x, i = rb / a.hb, h = 16 * (rb - i * a.hb) + n16;
-            ok = i <= p.k && h < p.Hq;
-            return ((int64_t)b * (p.k + 1) + (i <= p.k ? i : p.k)) * p.Hq + (h < p.Hq ? h : p.Hq - 1);
+        auto row_of = [&](int x, int n16, bool &ok) {
+            cLatent *A = arguments();
+            const int rb = u * NB + x, i = rb / A->hb, h = 16 * (rb - i * A->hb) + n16, k = A->p.k, Hq = A->p.Hq;
+            ok = i <= k && h < Hq;
+            return ((int64_t)b * (k + 1) + (i <= k ? i : k)) * Hq + (h < Hq ? h : Hq - 1);
         };
         f32x4 acc[XB][NB];
         float l[NW], msub[NW], thr[NW];  // of the rows this wave scores
@@ -200,24 +215,31 @@ __global__ __launch_bounds__(256, 1) void latent_mfma_kernel(Latent a) {
         if (n > 0) {
             // queries: step s of bf16 rows is dimensions 32 s + 8 j .. + 7; of fp8 rows, whose
             // 16-byte chunk feeds two steps, 64 (s / 2) + 16 j + 8 (s % 2) .. + 7
-            u32x4 q[NW][STEPS];
+            u32x4 q[NW][QR];
+            const int ln0 = here(lane);
 #pragma unroll
             for (int x = 0; x < NW; ++x) {
                 bool ok;
-                const uint8_t *row = p.q + row_of(NW * rw + x, ok) * (DK * 2) + (FP8 ? 32 : 16) * j;
+                const uint8_t *row = arguments()->p.q + row_of(NW * rw + x, ln0 & 15, ok) * (DK * 2) + (FP8 ? 32 : 16) * (ln0 >> 4);
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-                    q[x][s] = *reinterpret_cast<const u32x4 *>(row + (FP8 ? 128 * (s >> 1) + 16 * (s & 1) : 64 * s));
+                for (int s = 0; s < STEPS; ++s) {
+                    const u32x4 v = *reinterpret_cast<const u32x4 *>(row + (FP8 ? 128 * (s >> 1) + 16 * (s & 1) : 64 * s));
+                    if (s < QR) q[x][s] = v;
+                    else if (kw == 0)  // shared by the waves of these rows; the first tile's barrier publishes it
+                        *reinterpret_cast<lds_u32x4 *>((lds_u8 *)(uintptr_t)(q0 + 1024 * (NB * (s - QR) + x))) = v;
+                }
             }
 
             // copies of this wave's 16 rows of tile t into stage `st`
             const int last = t1 - 1;
             auto issue = [&](int st, int t) {
-                const uint32_t at = (uint32_t)(uintptr_t)(ring + st * G::BYTES) + (uint32_t)wave * 16 * G::RB;
-                const uint32_t rat = (uint32_t)(uintptr_t)(ring + st * G::BYTES) + G::MAIN + (uint32_t)wave * 16 * G::RR;
-                int key = t * kLatTile + 16 * wave;
-                if (a.uniform) {  // 16 rows in one run of storage
-                    key = key < n ? key : ((n - 1) & ~15);
+                const uint32_t at = (uint32_t)(uintptr_t)(ring + st * G::BYTES) + (uint32_t)wave * G::ROWS * G::RB;
+                const uint32_t rat = (uint32_t)(uintptr_t)(ring + st * G::BYTES) + G::MAIN + (uint32_t)wave * G::ROWS * G::RR;
+                int key = t * kLatTile + G::ROWS * wave;
+                const int r0 = (G::ROWS * wave) & 15;
+                const int lane = here(tid & 63);
+                if (a.uniform) {  // 16 keys in one run of storage
+                    key = key < n ? key : ((n - 1) & ~(G::ROWS - 1));
                     int64_t off;
                     int rmax = 15;
                     if (p.kv.page_size > 0) {
@@ -232,16 +254,17 @@ __global__ __launch_bounds__(256, 1) void latent_mfma_kernel(Latent a) {
                     const uint64_t base = (uint64_t)(uintptr_t)p.kv.k + (uint64_t)(off * G::ES);
                     auto go = [&](auto nt) {
                         constexpr bool NT = decltype(nt)::value;
-const uint32_t q16 = here(16u * (lane % G::CH)), rq16 = here(16u * (lane % G::RCH)), tb = here_s(tok_bytes);
+const uint32_t q16 = 16u * (lane % G::CH), rq16 = 16u * (lane % G::RCH), tb = here_s(tok_bytes);
 #pragma unroll
                         for (int x = 0; x < G::ML; ++x) {
                             const int r = x * (64 / G::CH) + (G::CH < 64 ? lane / G::CH : 0);
-                            copy16_s<NT>(base, (uint32_t)(r < rmax ? r : rmax) * tb + (q16 ^ (16u * fm(r))), at + x * 1024);
+                            copy16_s<NT>(base, (uint32_t)(r < rmax ? r : rmax) * tb + (q16 ^ (16u * fm(r0 + r))), at + x * 1024);
                         }
 #pragma unroll
                         for (int x = 0; x < G::RL; ++x) {
                             const int r = x * (64 / G::RCH) + lane / G::RCH;
-                            copy16_s<NT>(base, (uint32_t)(r < rmax ? r : rmax) * tb + G::RB + (rq16 ^ (16u * fr<FP8>(r))), rat + x * 1024);
+                            if (r < G::ROWS)
+                                copy16_s<NT>(base, (uint32_t)(r < rmax ? r : rmax) * tb + G::RB + (rq16 ^ (16u * fr<FP8>(r0 + r))), rat + x * 1024);
                         }
                     };
                     if (a.units == 1) go(std::true_type{});
@@ -249,7 +272,7 @@ const uint32_t q16 = here(16u * (lane % G::CH)), rq16 = here(16u * (lane % G::RC
                     return;
                 }
                 // any page size: lane r holds the address of row r
-                key += n16;
+                key += lane & (G::ROWS - 1);
                 key = key < n ? key : n - 1;
                 const uint32_t idx = (uint32_t)key / (uint32_t)p.kv.page_size;
                 int page = p.kv.block_table[(int64_t)b * p.kv.max_blocks + idx];
@@ -257,15 +280,16 @@ const uint32_t q16 = here(16u * (lane % G::CH)), rq16 = here(16u * (lane % G::RC
                 const uint64_t addr = (uint64_t)(uintptr_t)p.kv.k +
                     (uint64_t)(((int64_t)page * p.kv.s_blk + (int64_t)(key - (int)idx * p.kv.page_size) * p.kv.s_tok) * G::ES);
 const uint32_t ln = here(lane);
-#pragma unroll
+#pragma unroll 1
                 for (int x = 0; x < G::ML; ++x) {
-                    const int r = x * (64 / G::CH) + ln / G::CH, q16 = (ln % G::CH) ^ fm(r);
+                    const int r = x * (64 / G::CH) + lane / G::CH, q16 = (lane % G::CH) ^ fm(r0 + r);
                     copy16_v<false>(__shfl(addr, r) + 16u * q16, at + x * 1024);
                 }
-#pragma unroll
+#pragma unroll 1
                 for (int x = 0; x < G::RL; ++x) {
-                    const int r = x * (64 / G::RCH) + ln / G::RCH, q16 = (ln % G::RCH) ^ fr<FP8>(r);
-                    copy16_v<false>(__shfl(addr, r) + G::RB + 16u * q16, rat + x * 1024);
+                    const int r = x * (64 / G::RCH) + lane / G::RCH, q16 = (lane % G::RCH) ^ fr<FP8>(r0 + r);
+                    const uint64_t from = __shfl(addr, r) + G::RB + 16u * q16;
+                    if (r < G::ROWS) copy16_v<false>(from, rat + x * 1024);
                 }
             };
 
@@ -284,29 +308,23 @@ const uint32_t ln = here(lane);
                 const int key0 = tt * kLatTile;
 
                 // ---- S^T of this wave's keys and rows ------------------------------
-                f32x4 s[KB][NW], s2[KB][NW];
+                f32x4 s[NW], s2 = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int y = 0; y < KB; ++y)
-#pragma unroll
-                    for (int x = 0; x < NW; ++x) s[y][x] = s2[y][x] = f32x4{0.f, 0.f, 0.f, 0.f};
-                constexpr bool TWO = KB * NW == 1;  // one chain of dependent products: make it two
+                for (int x = 0; x < NW; ++x) s[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+                constexpr bool TWO = NW == 1;  // one chain of dependent products: make it two
                 // K operands a group of reads ahead of the products
-                constexpr int RAWS = FP8 ? STEPS / 2 : STEPS, READS = KB * RAWS;  // 16-byte reads
-                constexpr int KG = NW >= 3 ? 3 : 4;
-                auto read_k = [&](int i) {
-                    const int c = i / KB, y = i % KB;
-                    if constexpr (FP8)
-                        return lds_read<u32x4>(c < DC / 64 ? (kmain ^ (64 * (c & 3))) + 256 * (c >> 2) + 16 * y * G::RB
-                                                           : krope + 16 * y * G::RR);
-                    else
-                        return lds_read<u32x4>(c < DC / 32 ? (kmain ^ (64 * (c & 3))) + 256 * (c >> 2) + 16 * y * G::RB
-                                                           : (krope ^ (64 * (c - DC / 32))) + 16 * y * G::RR);
+                constexpr int READS = FP8 ? STEPS / 2 : STEPS;  // 16-byte reads
+                constexpr int KG = WAVES == 4 ? (NW >= 3 ? 3 : 4) : (FP8 ? 2 : 1);
+                auto read_k = [&](int c) {
+                    if constexpr (FP8) return lds_read<u32x4>(c < DC / 64 ? (kmain ^ (64 * (c & 3))) + 256 * (c >> 2) : krope);
+                    else return lds_read<u32x4>(c < DC / 32 ? (kmain ^ (64 * (c & 3))) + 256 * (c >> 2) : krope ^ (64 * (c - DC / 32)));
                 };
-                auto step = [&](int c, int y, u32x4 k4) {
+                auto step = [&](int c, u32x4 k4) {
 #pragma unroll
                     for (int x = 0; x < NW; ++x) {
-                        if (TWO && (c & 1)) s2[y][x] = mfma_bf16(k4, q[x][c], s2[y][x]);
-                        else s[y][x] = mfma_bf16(k4, q[x][c], s[y][x]);
+                        const u32x4 qx = c < QR ? q[x][c] : lds_read<u32x4>(q0 + 1024 * (NB * (c - QR) + x));
+                        if (TWO && (c & 1)) s2 = mfma_bf16(k4, qx, s2);
+                        else s[x] = mfma_bf16(k4, qx, s[x]);
                     }
                 };
                 u32x4 kb[2][KG];
@@ -322,61 +340,49 @@ const uint32_t ln = here(lane);
                     for (int y = 0; y < KG; ++y)
                         if (i0 + y < READS) {
                             const u32x4 r = kb[cur][y];
-                            const int c = (i0 + y) / KB, kk = (i0 + y) % KB;
                             if constexpr (FP8) {
-                                step(2 * c, kk, fp8x8_to_bf16x8(r.x, r.y));
-                                step(2 * c + 1, kk, fp8x8_to_bf16x8(r.z, r.w));
+                                step(2 * (i0 + y), fp8x8_to_bf16x8(r.x, r.y));
+                                step(2 * (i0 + y) + 1, fp8x8_to_bf16x8(r.z, r.w));
                             } else {
-                                step(c, kk, r);
+                                step(i0 + y, r);
                             }
                         }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if (TWO) s[0][0] += s2[0][0];
+                if (TWO) s[0] += s2;
 
                 // ---- mask, probabilities against the current references -----------
                 const bool tail = key0 + kLatTile > least;
                 if (tail) {
+                    const int key = key0 + 16 * kw + 4 * (here(lane) >> 4);
 #pragma unroll
-                    for (int y = 0; y < KB; ++y)
+                    for (int x = 0; x < NW; ++x)
 #pragma unroll
-                        for (int x = 0; x < NW; ++x)
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (key0 + 16 * (KB * kw + y) + 4 * j + e >= lim[x]) s[y][x][e] = -INFINITY;
+                        for (int e = 0; e < 4; ++e)
+                            if (key + e >= lim[x]) s[x][e] = -INFINITY;
                 }
                 auto top = [&](int x) {  // NaN-propagating: a NaN score never passes a threshold
-                    float m = max3n(s[0][x][0], s[0][x][1], __builtin_elementwise_maximum(s[0][x][2], s[0][x][3]));
-#pragma unroll
-                    for (int y = 1; y < KB; ++y)
-                        m = max3n(m, __builtin_elementwise_maximum(s[y][x][0], s[y][x][1]),
-                                  __builtin_elementwise_maximum(s[y][x][2], s[y][x][3]));
-                    return m;
+                    return __builtin_elementwise_maximum(max3n(s[x][0], s[x][1], s[x][2]), s[x][3]);
                 };
                 float add[NW];
                 auto weigh = [&]() {
 #pragma unroll
                     for (int x = 0; x < NW; ++x) {
-                        add[x] = 0.f;
+                        float e[4];
 #pragma unroll
-                        for (int y = 0; y < KB; ++y) {
-                            float e[4];
-#pragma unroll
-                            for (int z = 0; z < 4; ++z) e[z] = fast_exp2((s[y][x][z] - msub[x]) * sc);
-                            add[x] += (e[0] + e[1]) + (e[2] + e[3]);
-                            const u32x2 v = {pack_p<FP8>(e[0], e[1]), pack_p<FP8>(e[2], e[3])};
-                            *reinterpret_cast<__attribute__((address_space(3))) u32x2 *>(
-                                (lds_u8 *)(uintptr_t)((pwrite0 ^ (32 * y)) + 2048 * x)) = v;
-                        }
+                        for (int z = 0; z < 4; ++z) e[z] = fast_exp2((s[x][z] - msub[x]) * sc);
+                        add[x] = (e[0] + e[1]) + (e[2] + e[3]);
+                        const u32x2 v = {pack_p<FP8>(e[0], e[1]), pack_p<FP8>(e[2], e[3])};
+                        *reinterpret_cast<__attribute__((address_space(3))) u32x2 *>((lds_u8 *)(uintptr_t)(pwrite0 + 2048 * x)) = v;
                     }
                 };
                 // A hidden key's probability is 0, which clears any finite value; what is not
-                // finite in this wave's 16 rows from the first hidden key on is looked for.
+                // finite in this wave's rows from the first hidden key on is looked for.
                 bool bad = false;
                 if (tail) {
-                    for (int i = lane; i < 16 * G::CH; i += 64)
-                        if (key0 + 16 * wave + i / G::CH >= least)
-                            bad |= any_nonfinite<FP8>(lds_read<u32x4>(st + wave * 16 * G::RB + 16 * i));
+                    for (int i = lane; i < G::ROWS * G::CH; i += 64)
+                        if (key0 + G::ROWS * wave + i / G::CH >= least)
+                            bad |= any_nonfinite<FP8>(lds_read<u32x4>(st + wave * G::ROWS * G::RB + 16 * i));
                 }
                 bool over = false;
 #pragma unroll
@@ -385,9 +391,15 @@ const uint32_t ln = here(lane);
                 weigh();
                 if (lane == 0) flags[wave] = word;
                 lds_barrier();
-                const int4 fl = *reinterpret_cast<const int4 *>(flags);
-                const int events = __builtin_amdgcn_readfirstlane(fl.x | fl.y | fl.z | fl.w);
+                int all = 0;
+#pragma unroll
+                for (int w = 0; w < WAVES; w += 4) {
+                    const int4 fl = *reinterpret_cast<const int4 *>(flags + w);
+                    all |= fl.x | fl.y | fl.z | fl.w;
+                }
+                const int events = __builtin_amdgcn_readfirstlane(all);
                 if (events & 1) {
+                    const int ln = here(lane), n16 = ln & 15, j = ln >> 4;
                     // some row's scores pass its reference: move the references of all waves
 #pragma unroll
                     for (int x = 0; x < NW; ++x) {
@@ -435,6 +447,7 @@ const uint32_t ln = here(lane);
                 for (int x = 0; x < NW; ++x) l[x] += add[x];
 
                 if (events & 2) {
+                    const int j = here(lane) >> 4;
                     // A value that is not finite makes its dimension NaN in the rows that see its
                     // key (the key's score is not finite either); then it is cleared.
                     const int stop = n < key0 + kLatTile ? n : key0 + kLatTile;
@@ -442,7 +455,7 @@ const uint32_t ln = here(lane);
                         const int r = key - key0;
 #pragma unroll
                         for (int y = 0; y < XB; ++y) {
-                            const int d = wave * (DC / 4) + 16 * y + 4 * j, byte = d * G::ES;
+                            const int d = wave * (DC / WAVES) + 16 * y + 4 * j, byte = d * G::ES;
                             const uint32_t at = st + r * G::RB + 16 * ((byte >> 4) ^ fm(r & 15)) + (byte & 15);
                             f32x4 nan;
 #pragma unroll
@@ -457,9 +470,9 @@ const uint32_t ln = here(lane);
                         }
                     }
                     lds_barrier();
-                    for (int i = lane; i < 16 * G::CH; i += 64)
-                        if (key0 + 16 * wave + i / G::CH >= least) {
-                            const uint32_t at = st + wave * 16 * G::RB + 16 * i;
+                    for (int i = lane; i < G::ROWS * G::CH; i += 64)
+                        if (key0 + G::ROWS * wave + i / G::CH >= least) {
+                            const uint32_t at = st + wave * G::ROWS * G::RB + 16 * i;
                             if (any_nonfinite<FP8>(lds_read<u32x4>(at)))
                                 for (int e = 0; e < 16; e += G::ES)
                                     if (FP8 ? (lds_read<uint8_t>(at + e) & 0x7F) == 0x7F : (lds_read<uint16_t>(at + e) & 0x7F80) == 0x7F80) {
@@ -493,7 +506,7 @@ const uint32_t ln = here(lane);
                     if constexpr (FP8) return fp8x8_to_f16x8(r.x, r.y);
                     else return r;
                 };
-                constexpr int VG = 4;  // operands a group ahead
+                constexpr int VG = WAVES == 4 ? 4 : 1;  // operands a group ahead
                 decltype(read_v(0)) vb[2][VG];
                 u32x4 pf[NB];
 #pragma unroll
@@ -523,6 +536,7 @@ const uint32_t ln = here(lane);
         }
 
         // ---- row sums over the waves, rows out -------------------------------------
+        const int ln = here(lane), n16 = ln & 15, j = ln >> 4;
         lds_barrier();
 #pragma unroll
         for (int x = 0; x < NW; ++x) {
@@ -531,6 +545,7 @@ const uint32_t ln = here(lane);
             if (j == 0) red[kw * 16 * NB + 16 * (NW * rw + x) + n16] = l[x];
         }
         lds_barrier();
+        cLatent *A = arguments();
         const bool whole = tile == 0 && t1 == tiles;
         const int64_t slot = 2 * (int64_t)g + (pos == begin ? 0 : 1);
 #pragma unroll
@@ -541,25 +556,25 @@ const uint32_t ln = here(lane);
             const float inv = sum == 0.f ? 0.f : vscale / sum;
             const float lse2 = sum == 0.f ? -INFINITY : refs[16 * x + n16] * sc + log2f(sum);
             bool ok;
-            const int64_t qrow = row_of(x, ok);
+            const int64_t qrow = row_of(x, n16, ok);
             if (whole && !ok) continue;
-            const int64_t row = whole ? qrow : slot * pl.rows + 16 * (u * NB + x) + n16;
-            const int64_t at = row * DC + wave * (DC / 4) + 4 * j;
-            if (whole && p.out_dtype == SPIRE_BF16) {
-                uint16_t *o = static_cast<uint16_t *>(p.out) + at;
+            const int64_t row = whole ? qrow : slot * A->pl.rows + 16 * (u * NB + x) + n16;
+            const int64_t at = row * DC + wave * (DC / WAVES) + 4 * j;
+            if (whole && A->p.out_dtype == SPIRE_BF16) {
+                uint16_t *o = static_cast<uint16_t *>(A->p.out) + at;
 #pragma unroll
                 for (int y = 0; y < XB; ++y) {
                     const f32x4 v = acc[y][x] * inv;
                     *reinterpret_cast<u32x2 *>(o + 16 * y) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
                 }
             } else {
-                float *o = (whole ? static_cast<float *>(p.out) : pl.part_o) + at;
+                float *o = (whole ? static_cast<float *>(A->p.out) : A->pl.part_o) + at;
 #pragma unroll
                 for (int y = 0; y < XB; ++y) *reinterpret_cast<f32x4 *>(o + 16 * y) = acc[y][x] * inv;
             }
             if (wave == 0 && j == 0) {
-                if (!whole) pl.part_lse[row] = lse2;
-                else if (p.lse != nullptr) p.lse[row] = lse2 * 0.69314718055994531f;
+                if (!whole) A->pl.part_lse[row] = lse2;
+                else if (A->p.lse != nullptr) A->p.lse[row] = lse2 * 0.69314718055994531f;
             }
         }
         pos += te - tile;
@@ -570,12 +585,12 @@ const uint32_t ln = here(lane);
 
 template <int DC, bool FP8>
 static hipError_t launch_nb(const Latent &a, hipStream_t st) {
-    const dim3 grid((unsigned)(a.pl.workers * a.units)), block(256);
+    const dim3 grid((unsigned)(a.pl.workers * a.units));
     switch (a.nb) {
-    case 1: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 1>), grid, block, 0, st, a); break;
-    case 2: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 2>), grid, block, 0, st, a); break;
-    case 3: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 3>), grid, block, 0, st, a); break;
-    case 4: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 4>), grid, block, 0, st, a); break;
+    case 1: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 1, 4>), grid, dim3(256), 0, st, a); break;
+    case 2: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 2, 8>), grid, dim3(512), 0, st, a); break;
+    case 3: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 3, 4>), grid, dim3(256), 0, st, a); break;
+    case 4: hipLaunchKernelGGL((latent_mfma_kernel<DC, FP8, 4, 8>), grid, dim3(512), 0, st, a); break;
     default: return hipErrorInvalidValue;
     }
     return hipGetLastError();
