@@ -1020,10 +1020,10 @@ spire_status spire_latent_append(const void *c_new, int64_t c_stride, const void
 // Blocks per unit and groups of a launch (latent_common.h).
 struct LatentShape { int nb, units, groups; };
 
-// The matrix kernel holds up to 4 blocks, evenly spread over the units (5 blocks:
-// 3 + 2), the fp32 kernel one.
+// The matrix kernel holds up to 8 blocks, evenly spread over the units (10 blocks:
+// 5 + 5), the fp32 kernel one.
 static LatentShape latent_shape(int Hq, int k, int cus, bool matrix) {
-    const int blocks = (k + 1) * ((Hq + 15) / 16), most = matrix ? 4 : 1;
+    const int blocks = (k + 1) * ((Hq + 15) / 16), most = matrix ? 8 : 1;
     LatentShape s;
     s.units = (blocks + most - 1) / most;
     s.nb = (blocks + s.units - 1) / s.units;
@@ -1117,13 +1117,14 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
     a.nb = sh.nb;
     a.units = sh.units;
     a.uniform = latent->page_size % 16 == 0;
+    a.ps_shift = latent->page_size > 0 && (latent->page_size & (latent->page_size - 1)) == 0 ? __builtin_ctz((unsigned)latent->page_size) : -1;
     a.quads = (uintptr_t)latent->c % (4 * es) == 0 && latent->s_blk % 4 == 0 && latent->s_tok % 4 == 0;
     Plan &pl = a.pl;
-    pl.tile = matrix ? 64 : 32;
+    pl.tile = matrix ? latent_tile(p.D, es == 1) : 32;
     pl.units = 1;
     pl.rows = sh.units * sh.nb * 16;
     pl.workers = sh.groups;
-    pl.seg_cost = matrix ? 2 : 0;
+    pl.seg_cost = matrix ? 6 : 0;
     const Layout L = latent_layout(B, p.D, sh);
     if (workspace_bytes < L.total)
         return fail(SPIRE_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, L.total);
