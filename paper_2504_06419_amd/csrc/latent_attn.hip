@@ -15,7 +15,7 @@ namespace spire {
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kLatF32Tile = 32;
+constexpr int kLatF32Tile = kLatentTile;
 
 __device__ __forceinline__ float e4m3fn_f32(uint32_t x) {
     return __builtin_amdgcn_cvt_f32_fp8((int)x, 0);

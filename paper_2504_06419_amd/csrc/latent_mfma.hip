@@ -5,22 +5,24 @@
 // NB <= 8 blocks of 16 query rows and walks tiles of 16 KT keys, copied HBM -> LDS by
 // the load-to-LDS instructions into a ring of stages.  A row is key and value at
 // once, so one copy of it in LDS feeds both products:
-//   S^T = K Q^T     wave w scores all keys of the tile for row block w, whose
-//                   queries stay in its registers, and owns the block's softmax;
+//   S^T = K Q^T     waves 2 i and 2 i + 1 score all keys of the tile for row blocks
+//                   2 i and 2 i + 1, each over half of the dimensions (every other 16-byte
+//                   chunk group), queries in registers; they swap the halves that
+//                   the other needs through LDS, and each owns one block's softmax;
 //   O^T += C^T P^T  every wave takes an eighth of the latent's dimensions of all
 //                   rows, C^T by transposing LDS reads, P through LDS.
-// The products of a tile are a tile apart: between two barriers a wave scores tile
-// t + 1 and accumulates tile t, so that while one wave of a SIMD forms
-// probabilities the other feeds the matrix pipe, and one barrier a tile orders
-// the ring, P and the rescaling factors.
+// The products of a tile are a tile apart: after tile t + 1 is scored and the halves
+// are swapped, a wave forms its probabilities and accumulates tile t, so that one
+// wave of a SIMD feeds the matrix pipe while the other takes exponentials.
 //
 // Why this split.  A CU takes some 30 GB/s from L2, whether the lines are there or
 // not (8 units of 64 rows that share their keys in L2: 2.4 us a tile of 64 keys
 // without any arithmetic), so rows that share keys belong into one workgroup: 128
 // rows are what its registers hold (128 accumulators and 72 queries of 256).
-// LDS then delivers (NB 36 + 8 (4 + NB)) 16-byte reads for (NB 36 + 8 NB 4) matrix
-// instructions of a 32-key tile of 512 dimensions, at 8 rows 3072 cycles beside
-// 2176 of the matrix pipes.
+// A K operand read from LDS serves two row blocks, so LDS delivers 272 16-byte reads
+// (2176 cycles) for the 272 matrix instructions a SIMD issues (2176) on a 32-key tile
+// of 512 dimensions and 128 rows; with a wave per block and all dimensions it is 384
+// (measured without copies: 2.4 us a tile).
 #include <type_traits>
 
 #include "latent_common.h"
@@ -35,20 +37,21 @@ typedef int s32x2 __attribute__((ext_vector_type(2)));
 // Load-to-LDS of 16 bytes per lane: lane L's bytes land at lds + 16 L.  Written as
 // assembly because the compiler orders its transposing LDS reads behind every
 // load-to-LDS that it knows of (vmcnt(0)), which would drain the ring each tile; the
-// waits are the kernel's own.  No register is written; m0 names the LDS address.
+// waits are the kernel's own.  No register is written but m0, the LDS address,
+// which the compiler sets anew for each use of its own.
 template <bool NT>
 __device__ __forceinline__ void copy16_s(uint64_t base, uint32_t off, uint32_t lds) {
     if constexpr (NT)
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(lds) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
 }
 template <bool NT>
 __device__ __forceinline__ void copy16_v(uint64_t addr, uint32_t lds) {
     if constexpr (NT)
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(addr), "s"(lds) : "memory", "m0");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(addr), "s"(lds) : "memory");
     else
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds) : "memory", "m0");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds) : "memory");
 }
 
 // Workgroup barrier for LDS contents: this wave's LDS accesses are complete; copies
@@ -84,6 +87,14 @@ template <class V> __device__ __forceinline__ V lds_read(uint32_t at) {
 template <bool FP8> __device__ __forceinline__ bool not_finite(uint32_t at) {
     return FP8 ? (lds_read<uint8_t>(at) & 0x7F) == 0x7F : (lds_read<uint16_t>(at) & 0x7F80) == 0x7F80;
 }
+// Registers that loads fill: has the compiler wait for them here.  Without it the
+// wait stands at their first use in the tile loop and, taken every time round,
+// also waits for the copies in flight.
+template <int N> __device__ __forceinline__ void settle(u32x4 (&r)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(r[i]));
+}
+
 // The kernel's arguments, read again from where it is called: what is used once per
 // segment does not occupy scalar registers through the tile loop.
 typedef const Latent __attribute__((address_space(4))) cLatent;
@@ -93,20 +104,19 @@ __device__ __forceinline__ cLatent *arguments() {
     return (cLatent *)x;
 }
 
-// 16-key blocks a tile: as many bytes in every form, about 36 KB.
-constexpr int latent_kt(int Dc, bool fp8) { return Dc == 512 && !fp8 ? 2 : 4; }
+constexpr int kLatKT = kLatentTile / 16;  // 16-key blocks a tile
 
 // Stage of one tile: [TILE][DC] rows, then [TILE][64] rotated parts.  16-byte chunk q of
 // row r lies at q ^ fm(r) (main part, low 4 bits) and q ^ fr(r): operand reads (16
 // rows, one chunk) and transposing reads (4 rows, 2 chunks) hit distinct banks.
-template <int DC, bool FP8> struct LatStage {
-    static constexpr int KT = latent_kt(DC, FP8), TILE = 16 * KT;
+template <int DC, bool FP8, int CW> struct LatStage {  // CW: waves that copy
+    static constexpr int KT = kLatKT, TILE = 16 * KT;
     static constexpr int ES = FP8 ? 1 : 2;
     static constexpr int RB = DC * ES, RR = kLatentDr * ES;  // bytes of a row's parts
     static constexpr int MAIN = TILE * RB;
     static constexpr int BYTES = TILE * (RB + RR);
     static constexpr int CH = RB / 16, RCH = RR / 16;        // chunks of a row's parts
-    static constexpr int ROWS = TILE / 8;                    // rows a wave copies
+    static constexpr int ROWS = TILE / CW;                   // rows a copying wave takes
     static constexpr int ML = ROWS * CH / 64, RL = (ROWS * RCH + 63) / 64;  // its copies
     static constexpr int LOADS = ML + RL;
     static constexpr int PR = 2 * TILE;                      // bytes of a row of P
@@ -118,22 +128,33 @@ template <int PR> __device__ __forceinline__ int fp(int r) { return PR == 64 ? (
 
 template <int DC, bool FP8, int NB>
 __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
-    using G = LatStage<DC, FP8>;
+    // Waves without rows to score copy the tiles; with 7 and 8 blocks every wave does its share.
+    constexpr int CW = NB <= 4 ? 4 : (NB <= 6 ? 2 : 8), SCAN = kLatentTile / 8;  // copying waves; rows a wave looks through
+    using G = LatStage<DC, FP8, CW>;
+    constexpr bool NT = NB <= 4;  // up to 4 blocks are one unit: its rows are read once, and streamed
     constexpr int DK = DC + kLatentDr, TILE = G::TILE, KT = G::KT;
     constexpr int STEPS = DK / 32;      // QK steps of 32 dimensions
     constexpr int XB = DC / 128;        // 16-dimension output blocks of a wave
     constexpr int PB = NB * 16 * G::PR;
-    constexpr int REST = 2 * PB + 2 * NB * 64 + 64;
-    constexpr int NS0 = (160 * 1024 - REST) / G::BYTES, NS = NS0 > 6 ? 6 : NS0;
+    constexpr int REST = 3 * PB + 2 * NB * 64 + 64;  // P twice, what the halves take beyond one of them
+    // Queries (see below).  With 7 and 8 blocks of a 512-wide latent the registers run out: the
+    // last group's queries lie in LDS, each lane's in a place of its own.
+    constexpr int GROUPS = FP8 ? STEPS / 2 : STEPS, HG = (GROUPS + 1) / 2;  // 16-byte groups of a row, of a wave
+    constexpr int QB = NB == 1 ? 1 : 2, QS = FP8 ? 2 : 1;                   // blocks, steps a group
+    constexpr bool QL = DC == 512 && NB >= 7;
+    constexpr int QR = QL ? HG - 1 : HG, QBYTES = QL ? 8 * QB * QS * 1024 : 0;
+    constexpr int NS0 = (160 * 1024 - REST - QBYTES) / G::BYTES, NS = NS0 > 6 ? 6 : NS0;
     static_assert(NS >= 3, "stage ring too small");
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * G::BYTES + REST];
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[NS * G::BYTES + REST + QBYTES];
     lds_u8 *ring = (lds_u8 *)smem;
-    float *alphas = reinterpret_cast<float *>(smem + NS * G::BYTES + 2 * PB);  // [2][16 NB]; at the end sums, references
-    int *flags = reinterpret_cast<int *>(smem + NS * G::BYTES + 2 * PB + 2 * NB * 64);  // [2][8]
+    float *alphas = reinterpret_cast<float *>(smem + NS * G::BYTES + 3 * PB);  // [2][16 NB]; at the end sums, references
+    int *flags = reinterpret_cast<int *>(smem + NS * G::BYTES + 3 * PB + 2 * NB * 64);  // [2][8]
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const bool scorer = wave < NB;
+    const int half = wave & 1, cw = wave - (8 - CW);
+    const bool copier = cw >= 0;
+    const bool pair = wave < ((NB + 1) & ~1), owner = wave < NB;  // scores, owns row block `wave`
     const int n16 = lane & 15, j = lane >> 4;
     const Problem &p = a.p;
     const Plan &pl = a.pl;
@@ -151,13 +172,14 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
         vscale = uload(p.kv.k_scale, 0);
         sc *= vscale;
     }
-    const float margin = kRescaleLog2 / sc;  // of raw scores
+    const float margin = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(kRescaleLog2 / sc)));  // of raw scores
 
     // lane constants of the LDS accesses
     // (chunk 4 c + j of a row at 16 ((4 c + j) ^ f): only bits 4-7 of the address change with c & 3)
     const uint32_t ring0 = (uint32_t)(uintptr_t)ring;
-    const uint32_t kmain0 = ring0 + n16 * G::RB + 16 * (j ^ fm(n16));
-    const uint32_t krope0 = ring0 + G::MAIN + n16 * G::RR + 16 * (j ^ fr<FP8>(n16));
+    // a wave of a pair takes chunk groups c = 2 i + half
+    const uint32_t kmain0 = ring0 + n16 * G::RB + ((16 * (j ^ fm(n16))) ^ (64 * half));
+    const uint32_t krope0 = ring0 + G::MAIN + n16 * G::RR + ((16 * (j ^ fr<FP8>(n16))) ^ (FP8 ? 0 : 64 * half));
     // transposing reads: bf16: lane s of group j addresses key 8 j + 4 h + s / 4, 4 dimensions, and receives
     // dimension s of the group's 4 keys; fp8: key 8 j + s / 2, 8 dimensions, and receives dimension s of 8 keys
     const int vr = FP8 ? 8 * j + (n16 >> 1) : 8 * j + (n16 >> 2);
@@ -165,6 +187,9 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
     const uint32_t p0 = ring0 + NS * G::BYTES + n16 * G::PR;
     const uint32_t pread0 = p0 + 16 * (j ^ fp<G::PR>(n16));
     const uint32_t pwrite0 = p0 + 16 * G::PR * wave + 16 * ((j >> 1) ^ fp<G::PR>(n16)) + 8 * (j & 1);
+    // halves of a block's scores, 16 bytes a lane and 16 keys: in the block's P of the same tile, then behind both P
+    const uint32_t x0 = ring0 + NS * G::BYTES + 16 * G::PR * wave;  // + 16 lane
+    const uint32_t q0 = ring0 + NS * G::BYTES + REST + QB * QS * 1024 * wave;  // + 16 lane
     const uint32_t tok_bytes = (uint32_t)(p.kv.s_tok * G::ES);
 
     while (pos < end) {
@@ -203,47 +228,58 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
             for (int y = 0; y < XB; ++y) acc[y][x] = f32x4{0.f, 0.f, 0.f, 0.f};
         lds_barrier();  // every wave is done with the previous segment's LDS
         if (n > 0) {
-            // Copies of this wave's rows of a tile.  Where the rows lie in one run of storage
-            // its address is looked up a tile ahead.
+            // Copies of this wave's rows of a tile.  Where the rows lie in one run of storage,
+            // the lanes hold the runs' addresses for 64 tiles, formed at once (a scalar load
+            // per tile would hold up the LDS reads behind it).
             const int last = t1 - 1;
-            uint64_t from = 0, ahead = 0;
-            int rmax = G::ROWS - 1, rmax_ahead = G::ROWS - 1;
-            auto look_up = [&](int t) {  // into `ahead`; what was there becomes `from`
-                from = ahead;
-                rmax = rmax_ahead;
-                int key = t * TILE + G::ROWS * wave;
-                key = key < n ? key : ((n - 1) & ~(G::ROWS - 1));
-                int64_t off;
-                if (p.kv.page_size > 0) {
-                    const uint32_t idx = a.ps_shift >= 0 ? (uint32_t)key >> a.ps_shift : (uint32_t)key / (uint32_t)p.kv.page_size;
-                    int page = uload(p.kv.block_table, (int64_t)b * p.kv.max_blocks + idx);
-                    page = page < 0 ? 0 : (page >= p.kv.num_blocks ? p.kv.num_blocks - 1 : page);
-                    off = (int64_t)page * p.kv.s_blk + (int64_t)(key - (int)idx * p.kv.page_size) * p.kv.s_tok;
-                } else {
-                    off = (int64_t)b * p.kv.s_blk + (int64_t)key * p.kv.s_tok;
-                    rmax_ahead = p.kv.capacity - 1 - key;  // >= 0: key < n <= capacity
+            uint64_t from = 0;
+            uint32_t runs_lo = 0, runs_hi = 0;  // lane i: of tile held + i
+            int rmax = G::ROWS - 1, held = -64;
+            auto look_up = [&](int t) {
+                if (t >= held + 64) {
+                    held = t;
+                    int key = (t + (int)here(lane)) * TILE + G::ROWS * cw;
+                    key = key < n ? key : ((n - 1) & ~(G::ROWS - 1));
+                    int64_t blk = b;
+                    if (p.kv.page_size > 0) {
+                        const uint32_t idx = (uint32_t)key / (uint32_t)p.kv.page_size;
+                        const int page = p.kv.block_table[(int64_t)b * p.kv.max_blocks + idx];
+                        blk = page < 0 ? 0 : (page >= p.kv.num_blocks ? p.kv.num_blocks - 1 : page);
+                        key -= (int)idx * p.kv.page_size;
+                    }
+                    const uint64_t run = (uint64_t)(uintptr_t)p.kv.k + (uint64_t)((blk * p.kv.s_blk + (int64_t)key * p.kv.s_tok) * G::ES);
+                    runs_lo = (uint32_t)run;
+                    runs_hi = (uint32_t)(run >> 32);
+                    asm volatile("" : "+v"(runs_lo), "+v"(runs_hi));  // the wait for the page ids stands here
                 }
-                ahead = (uint64_t)(uintptr_t)p.kv.k + (uint64_t)(off * G::ES);
+                from = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(runs_lo, t - held) |
+                       (uint64_t)(uint32_t)__builtin_amdgcn_readlane(runs_hi, t - held) << 32;
+                if (p.kv.page_size == 0) {
+                    int key = t * TILE + G::ROWS * cw;
+                    key = key < n ? key : ((n - 1) & ~(G::ROWS - 1));
+                    rmax = p.kv.capacity - 1 - key;  // >= 0: key < n <= capacity
+                }
             };
-            const int r0 = (G::ROWS * wave) & 15;
+            const int r0 = (G::ROWS * cw) & 15;
             auto copy = [&](int st, int x) {  // copy x of ML + RL into stage st
-                const int lane = here(tid & 63);
+                const uint32_t lane = here(tid & 63);
                 const bool main = x < G::ML;
                 const int y = main ? x : x - G::ML, ch = main ? G::CH : G::RCH;
-                const int r = y * (64 / ch) + (ch < 64 ? lane / ch : 0);
-                const uint32_t chunk = (uint32_t)(lane % ch) ^ (main ? fm(r0 + r) : fr<FP8>(r0 + r));
+                const int r = y * (64 / ch) + (ch < 64 ? (int)(lane / ch) : 0);
+                const uint32_t chunk = lane % ch ^ (main ? fm(r0 + r) : fr<FP8>(r0 + r));
                 const uint32_t off = (uint32_t)(r < rmax ? r : rmax) * tok_bytes + (main ? 0 : G::RB) + 16 * chunk;
                 const uint32_t at = ring0 + st * G::BYTES + 1024 * y +
-                                    (main ? wave * G::ROWS * G::RB : G::MAIN + wave * G::ROWS * G::RR);
-                if (main || G::ROWS * G::RCH >= 64 || r < G::ROWS) {
-                    if (a.units == 1) copy16_s<true>(from, off, at);
-                    else copy16_s<false>(from, off, at);
-                }
+                                    (main ? cw * G::ROWS * G::RB : G::MAIN + cw * G::ROWS * G::RR);
+                if (main || G::ROWS * G::RCH >= 64 || r < G::ROWS) copy16_s<NT>(from, off, at);
+            };
+            auto copy_all = [&](int st) {
+#pragma unroll
+                for (int x = 0; x < G::LOADS; ++x) copy(st, x);
             };
             // any page size: lane r holds the address of row r
             auto copy_scattered = [&](int st, int t) {
                 const int lane = here(tid & 63);
-                int key = t * TILE + G::ROWS * wave + (lane & (G::ROWS - 1));
+                int key = t * TILE + G::ROWS * cw + (lane & (G::ROWS - 1));
                 key = key < n ? key : n - 1;
                 const uint32_t idx = (uint32_t)key / (uint32_t)p.kv.page_size;
                 int page = p.kv.block_table[(int64_t)b * p.kv.max_blocks + idx];
@@ -254,41 +290,118 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
 #pragma unroll 1
                 for (int x = 0; x < G::ML; ++x) {
                     const int r = x * (64 / G::CH) + lane / G::CH, q16 = (lane % G::CH) ^ fm(r0 + r);
-                    copy16_v<false>(__shfl(addr, r) + 16u * q16, at + wave * G::ROWS * G::RB + x * 1024);
+                    copy16_v<false>(__shfl(addr, r) + 16u * q16, at + cw * G::ROWS * G::RB + x * 1024);
                 }
 #pragma unroll 1
                 for (int x = 0; x < G::RL; ++x) {
                     const int r = x * (64 / G::RCH) + lane / G::RCH, q16 = (lane % G::RCH) ^ fr<FP8>(r0 + r);
                     const uint64_t src = __shfl(addr, r) + G::RB + 16u * q16;
-                    if (r < G::ROWS) copy16_v<false>(src, at + G::MAIN + wave * G::ROWS * G::RR + x * 1024);
+                    if (r < G::ROWS) copy16_v<false>(src, at + G::MAIN + cw * G::ROWS * G::RR + x * 1024);
                 }
             };
             auto issue = [&](int st, int t) {
-                if (!a.uniform) return copy_scattered(st, t);
-#pragma unroll
-                for (int x = 0; x < G::LOADS; ++x) copy(st, x);
+                if (a.uniform) copy_all(st);
+                else copy_scattered(st, t);
             };
 
-            if (a.uniform) look_up(tile);
-#pragma unroll
-            for (int s = 0; s < NS - 1; ++s) {
-                if (a.uniform) look_up(tile + s + 1);
-                if (tile + s <= last) issue(s, tile + s);
+            if (copier) {
+                for (int s = 0; s < NS - 1 && tile + s <= last; ++s) {
+                    if (a.uniform) look_up(tile + s);
+                    issue(s, tile + s);
+                }
             }
-            // queries: step s of bf16 rows is dimensions 32 s + 8 j .. + 7; of fp8 rows, whose
-            // 16-byte chunk feeds two steps, 64 (s / 2) + 16 j + 8 (s % 2) .. + 7
-            u32x4 q[STEPS];
-            {
+            // queries of the wave's own block and of its partner's: group c of bf16 rows is dimensions
+            // 32 c + 8 j .. + 7; of fp8 rows, whose 16-byte chunk feeds two steps, 64 c + 16 j .. + 15
+            u32x4 q[QB][QR * QS];
+            if (pair) {
                 const int ln = here(lane);
-                bool ok;
-                const uint8_t *row = arguments()->p.q + row_of(scorer ? wave : 0, ln & 15, ok) * (DK * 2) + (FP8 ? 32 : 16) * (ln >> 4);
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-                    q[s] = *reinterpret_cast<const u32x4 *>(row + (FP8 ? 128 * (s >> 1) + 16 * (s & 1) : 64 * s));
+                for (int x = 0; x < QB; ++x) {
+                    bool ok;
+                    const int block = NB == 1 ? 0 : wave ^ x;
+                    const uint8_t *row = arguments()->p.q + row_of(block < NB ? block : 0, ln & 15, ok) * (DK * 2) + (FP8 ? 32 : 16) * (ln >> 4);
+#pragma unroll
+                    for (int i = 0; i < HG; ++i)
+#pragma unroll
+                        for (int z = 0; z < QS; ++z) {
+                            const int c = 2 * i + half;
+                            u32x4 v = u32x4{0, 0, 0, 0};
+                            if (2 * i + 1 < GROUPS || half == 0)
+                                v = *reinterpret_cast<const u32x4 *>(row + (FP8 ? 128 : 64) * c + 16 * z);
+                            if (i < QR) q[x][i * QS + z] = v;
+                            else *reinterpret_cast<lds_u32x4 *>((lds_u8 *)(uintptr_t)(q0 + 1024 * (x * QS + z) + 16 * ln)) = v;
+                        }
+                }
             }
 
+#pragma unroll
+            for (int x = 0; x < QB; ++x) settle(q[x]);
+
+            // ---- half scores of tile t (stage st), the partner's sent to it -----------
+            // `more`: the copies of tile `next` go out between the products (from the waves
+            // that score: issued in a row they would stand in the way).
+            f32x4 s[QB][KT];
+            auto score = [&](int st, int buf, bool more, int into) {
+                if (CW < 8 && copier) {
+                    if (more) copy_all(into);
+                    return;
+                }
+                if (!pair) return;
+                const uint32_t kmain = here(kmain0 + st * G::BYTES), krope = here(krope0 + st * G::BYTES);
+#pragma unroll
+                for (int x = 0; x < QB; ++x)
+#pragma unroll
+                    for (int y = 0; y < KT; ++y) s[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+                // K operands a group of reads ahead of the products
+                constexpr int MG = FP8 ? DC / 64 : DC / 32;  // groups of the main part
+                auto read_k = [&](int i, int y) {
+                    return lds_read<u32x4>(2 * i < MG ? (kmain ^ (128 * (i & 1))) + 256 * (i >> 1) + 16 * y * G::RB : krope + 16 * y * G::RR);
+                };
+                u32x4 kb[2][KT];
+#pragma unroll
+                for (int y = 0; y < KT; ++y) kb[0][y] = read_k(0, y);
+#pragma unroll
+                for (int i = 0; i < HG; ++i) {
+                    if (i + 1 < HG) {
+#pragma unroll
+                        for (int y = 0; y < KT; ++y) kb[(i + 1) & 1][y] = read_k(i + 1, y);
+                    }
+#pragma unroll
+                    for (int y = 0; y < KT; ++y) {
+                        const u32x4 r = kb[i & 1][y];
+                        auto query = [&](int x, int z) {
+                            return i < QR ? q[x][i * QS + z] : lds_read<u32x4>(q0 + 1024 * (x * QS + z) + 16 * here(lane));
+                        };
+                        if constexpr (FP8) {
+                            const u32x4 lo = fp8x8_to_bf16x8(r.x, r.y), hi = fp8x8_to_bf16x8(r.z, r.w);
+#pragma unroll
+                            for (int x = 0; x < QB; ++x) {
+                                s[x][y] = mfma_bf16(lo, query(x, 0), s[x][y]);
+                                s[x][y] = mfma_bf16(hi, query(x, 1), s[x][y]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < QB; ++x) s[x][y] = mfma_bf16(r, query(x, 0), s[x][y]);
+                        }
+                    }
+                    if (CW == 8 && more) {
+#pragma unroll
+                        for (int x = 0; x < G::LOADS; ++x)
+                            if (x * HG / G::LOADS == i) copy(into, x);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if ((wave ^ 1) < NB) {
+                    const uint32_t at = x0 + (half ? -16 * G::PR : 16 * G::PR) + 16 * here(lane);  // the partner's block
+#pragma unroll
+                    for (int y = 0; y < KT; ++y)
+                        *reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(
+                            (lds_u8 *)(uintptr_t)(at + (y < KT / 2 ? buf * PB + 1024 * y : 2 * PB + 1024 * (y - KT / 2)))) = s[QB - 1][y];
+                }
+            };
+
             // ---- probabilities of tile t (stage st) into buffer `buf` ----------------
-            auto score = [&](int t, int st, int buf) {
+            auto weigh = [&](int t, int st, int buf) {
                 const int key0 = t * TILE;
                 const bool tail = key0 + TILE > least;
                 // A hidden key's probability is 0, which clears any finite value; what is not
@@ -296,67 +409,29 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
                 bool bad = false;
                 if (tail) {
                     const int lane = here(tid & 63);
-                    for (int i = lane; i < G::ROWS * G::CH; i += 64)
-                        if (key0 + G::ROWS * wave + i / G::CH >= least)
-                            bad |= any_nonfinite<FP8>(lds_read<u32x4>(ring0 + st * G::BYTES + wave * G::ROWS * G::RB + 16 * i));
+                    for (int i = lane; i < SCAN * G::CH; i += 64)
+                        if (key0 + SCAN * wave + i / G::CH >= least)
+                            bad |= any_nonfinite<FP8>(lds_read<u32x4>(ring0 + st * G::BYTES + wave * SCAN * G::RB + 16 * i));
                 }
                 int word = __any(bad) ? 2 : 0;
-                if (scorer) {
-                    const uint32_t kmain = here(kmain0 + st * G::BYTES), krope = here(krope0 + st * G::BYTES);
-                    f32x4 s[KT];
+                if (owner) {
+                    const uint32_t at = x0 + 16 * here(lane);
 #pragma unroll
-                    for (int y = 0; y < KT; ++y) s[y] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    // K operands a group of reads ahead of the products
-                    constexpr int RAWS = FP8 ? STEPS / 2 : STEPS, KG = 4 / KT;  // steps a group
-                    auto read_k = [&](int c, int y) {
-                        if constexpr (FP8)
-                            return lds_read<u32x4>((c < DC / 64 ? (kmain ^ (64 * (c & 3))) + 256 * (c >> 2) + 16 * y * G::RB : krope + 16 * y * G::RR));
-                        else
-                            return lds_read<u32x4>((c < DC / 32 ? (kmain ^ (64 * (c & 3))) + 256 * (c >> 2) + 16 * y * G::RB
-                                                                : (krope ^ (64 * (c - DC / 32))) + 16 * y * G::RR));
-                    };
-                    u32x4 kb[2][KG][KT];
-                    auto fetch = [&](int into, int c0) {
-#pragma unroll
-                        for (int c = 0; c < KG; ++c)
-#pragma unroll
-                            for (int y = 0; y < KT; ++y)
-                                if (c0 + c < RAWS) kb[into][c][y] = read_k(c0 + c, y);
-                    };
-                    fetch(0, 0);
-#pragma unroll
-                    for (int c0 = 0; c0 < RAWS; c0 += KG) {
-                        const int cur = (c0 / KG) & 1;
-                        fetch(cur ^ 1, c0 + KG);
-#pragma unroll
-                        for (int c = 0; c < KG; ++c)
-                            if (c0 + c < RAWS) {
-#pragma unroll
-                                for (int y = 0; y < KT; ++y) {
-                                    const u32x4 r = kb[cur][c][y];
-                                    if constexpr (FP8) {
-                                        s[y] = mfma_bf16(fp8x8_to_bf16x8(r.x, r.y), q[2 * (c0 + c)], s[y]);
-                                        s[y] = mfma_bf16(fp8x8_to_bf16x8(r.z, r.w), q[2 * (c0 + c) + 1], s[y]);
-                                    } else {
-                                        s[y] = mfma_bf16(r, q[c0 + c], s[y]);
-                                    }
-                                }
-                            }
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                    for (int y = 0; y < KT; ++y)
+                        s[0][y] += lds_read<f32x4>(at + (y < KT / 2 ? buf * PB + 1024 * y : 2 * PB + 1024 * (y - KT / 2)));
                     if (tail) {
                         const int key = key0 + 4 * (here(lane) >> 4);
 #pragma unroll
                         for (int y = 0; y < KT; ++y)
 #pragma unroll
                             for (int e = 0; e < 4; ++e)
-                                if (key + 16 * y + e >= lim) s[y][e] = -INFINITY;
+                                if (key + 16 * y + e >= lim) s[0][y][e] = -INFINITY;
                     }
                     // lazy references: a row's moves when a score passes it by more than 2^8
                     // (NaN-propagating maximum: a NaN score never passes)
-                    float top = s[0][0];
+                    float top = s[0][0][0];
 #pragma unroll
-                    for (int y = 0; y < KT; ++y) top = max3n(max3n(top, s[y][0], s[y][1]), s[y][2], s[y][3]);
+                    for (int y = 0; y < KT; ++y) top = max3n(max3n(top, s[0][y][0], s[0][y][1]), s[0][y][2], s[0][y][3]);
                     if (__any(top > thr)) {
                         float m = top != top ? -INFINITY : top;
                         m = fmaxf(m, __shfl_xor(m, 16));
@@ -376,7 +451,7 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
                     for (int y = 0; y < KT; ++y) {
                         float e[4];
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) e[z] = fast_exp2((s[y][z] - msub) * sc);
+                        for (int z = 0; z < 4; ++z) e[z] = fast_exp2((s[0][y][z] - msub) * sc);
                         l += (e[0] + e[1]) + (e[2] + e[3]);
                         const u32x2 v = {pack_p<FP8>(e[0], e[1]), pack_p<FP8>(e[2], e[3])};
                         *reinterpret_cast<__attribute__((address_space(3))) u32x2 *>((lds_u8 *)(uintptr_t)((pwrite0 ^ (32 * y)) + buf * PB)) = v;
@@ -395,19 +470,33 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
             };
             wait_vmcnt<0>();  // the queries and the first tiles
             lds_barrier();
-            score(tile, 0, 0);
+            score(0, 0, false, 0);
+            lds_barrier();
+            weigh(tile, 0, 0);
             int rd = 0, buf = 0, wr = NS - 1;
             for (int tt = tile; tt <= last; ++tt) {
                 landed(tt + 1);
                 lds_barrier();  // tile tt + 1 and the probabilities of tt are there, tile tt - 1 is read
-                if (a.uniform) look_up(tt + NS);
-                if (tt + NS - 1 <= last) issue(wr, tt + NS - 1);
+                const bool more = tt + NS - 1 <= last;
+                if (copier && more) {
+                    if (a.uniform) look_up(tt + NS - 1);
+                    else copy_scattered(wr, tt + NS - 1);
+                }
+                const int into = wr;
                 wr = wr + 1 == NS ? 0 : wr + 1;
                 const int st = rd, key0 = tt * TILE;
                 rd = rd + 1 == NS ? 0 : rd + 1;
-                const int4 f0 = *reinterpret_cast<const int4 *>(flags + 8 * buf), f1 = *reinterpret_cast<const int4 *>(flags + 8 * buf + 4);
-                if (tt < last) score(tt + 1, rd, buf ^ 1);
-                const int events = __builtin_amdgcn_readfirstlane(f0.x | f0.y | f0.z | f0.w | f1.x | f1.y | f1.z | f1.w);
+                if (tt < last) {
+                    score(rd, buf ^ 1, more && a.uniform, into);
+                    lds_barrier();  // the halves are there
+                }
+                int word = 0;
+                {
+                    const int4 f0 = *reinterpret_cast<const int4 *>(flags + 8 * buf), f1 = *reinterpret_cast<const int4 *>(flags + 8 * buf + 4);
+                    word = f0.x | f0.y | f0.z | f0.w | f1.x | f1.y | f1.z | f1.w;
+                }
+                if (tt < last) weigh(tt + 1, rd, buf ^ 1);
+                const int events = __builtin_amdgcn_readfirstlane(word);
 
                 // Accumulators change outside the products in this one place only (each place
                 // more costs the register allocator a copy of them).
@@ -436,9 +525,9 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
                             for (int x = 0; x < NB; ++x) nans[x] |= key < limit(x) ? bits : 0u;
                         }
                         lds_barrier();
-                        for (int i = lane; i < G::ROWS * G::CH; i += 64)
-                            if (key0 + G::ROWS * wave + i / G::CH >= least) {
-                                const uint32_t at = sb + wave * G::ROWS * G::RB + 16 * i;
+                        for (int i = lane; i < SCAN * G::CH; i += 64)
+                            if (key0 + SCAN * wave + i / G::CH >= least) {
+                                const uint32_t at = sb + wave * SCAN * G::RB + 16 * i;
                                 for (int e = 0; e < 16; e += G::ES)
                                     if (not_finite<FP8>(at + e)) {
                                         if constexpr (FP8) *reinterpret_cast<__attribute__((address_space(3))) uint8_t *>((lds_u8 *)(uintptr_t)(at + e)) = 0;
@@ -449,9 +538,7 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
                     }
 #pragma unroll
                     for (int x = 0; x < NB; ++x) {
-                        const int f = x == 0 ? f0.x : x == 1 ? f0.y : x == 2 ? f0.z : x == 3 ? f0.w
-                                    : x == 4 ? f1.x : x == 5 ? f1.y : x == 6 ? f1.z : f1.w;
-                        const float alpha = f & 1 ? alphas[buf * 16 * NB + 16 * x + (lane & 15)] : 1.f;  // the reference moved
+                        const float alpha = flags[8 * buf + x] & 1 ? alphas[buf * 16 * NB + 16 * x + (lane & 15)] : 1.f;  // the reference moved
 #pragma unroll
                         for (int y = 0; y < XB; ++y)
 #pragma unroll
@@ -502,7 +589,7 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
         lds_barrier();
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
-        if (scorer && j == 0) {
+        if (owner && j == 0) {
             alphas[16 * wave + n16] = l;
             alphas[16 * NB + 16 * wave + n16] = msub;
         }
@@ -542,8 +629,6 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
         tile = 0;
     }
 }
-
-int latent_tile(int Dc, bool fp8) { return 16 * latent_kt(Dc, fp8); }
 
 template <int DC, bool FP8>
 static hipError_t launch_nb(const Latent &a, hipStream_t st) {

@@ -1117,10 +1117,9 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
     a.nb = sh.nb;
     a.units = sh.units;
     a.uniform = latent->page_size % 16 == 0;
-    a.ps_shift = latent->page_size > 0 && (latent->page_size & (latent->page_size - 1)) == 0 ? __builtin_ctz((unsigned)latent->page_size) : -1;
     a.quads = (uintptr_t)latent->c % (4 * es) == 0 && latent->s_blk % 4 == 0 && latent->s_tok % 4 == 0;
     Plan &pl = a.pl;
-    pl.tile = matrix ? latent_tile(p.D, es == 1) : 32;
+    pl.tile = kLatentTile;
     pl.units = 1;
     pl.rows = sh.units * sh.nb * 16;
     pl.workers = sh.groups;

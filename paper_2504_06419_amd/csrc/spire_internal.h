@@ -315,6 +315,7 @@ hipError_t launch_qkv_append(const QkvAppend &x, hipStream_t st);
 hipError_t launch_latent_append(const LatentAppend &x, hipStream_t st);
 
 // ---- latent attention (latent_common.h, latent_attn.hip) ----------------------------
+constexpr int kLatentTile = 32;  // keys a tile, both kernels
 constexpr int kLatentDr = 64;  // rotated elements of a row
 struct Latent {
     Problem p;        // Hkv = 1, D = Dc, kv = the latent view (k, k_scale)
@@ -323,10 +324,8 @@ struct Latent {
     int32_t nb;       // blocks per unit
     int32_t units;    // units per sequence = workgroups per group
     int32_t quads;    // fp32 kernel: cache elements readable four at a time
-    int32_t ps_shift; // log2 of the page size, -1: not a power of two
     int32_t uniform;  // matrix kernel: 16 keys from a multiple of 16 on lie in one run of storage
 };
-int latent_tile(int Dc, bool fp8);  // keys a tile of the matrix kernel
 hipError_t launch_latent_mfma(const Latent &a, hipStream_t st);
 hipError_t launch_latent_f32(const Latent &a, hipStream_t st);
 hipError_t launch_latent_combine(const Latent &a, hipStream_t st);
