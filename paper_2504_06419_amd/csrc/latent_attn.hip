@@ -34,12 +34,9 @@ __global__ __launch_bounds__(256) void latent_f32_kernel(Latent a) {
     const Plan &pl = a.pl;
     int g, u;
     latent_place(a, g, u);
-    if (g >= pl.workers) return;
-    const int64_t T = (int64_t)uload(pl.prefix, p.B);
-    int64_t pos = worker_begin(g, T, pl.workers);
-    const int64_t end = worker_begin(g + 1, T, pl.workers);
-    if (pos >= end) return;
-    int seg = uload(pl.wstart, 2 * g), tile = uload(pl.wstart, 2 * g + 1);
+    int64_t pos = 0, end = 0;
+    int seg = 0, tile = 0;
+    if (!latent_start<256>(a, g, u, reinterpret_cast<int32_t *>(&ks[0][0]), seg, tile, pos, end)) return;
     const int64_t begin = pos;
     const int i = u / a.hb, h = 16 * (u - i * a.hb) + n16;  // units are single blocks here
     const bool row_ok = h < p.Hq;
@@ -47,13 +44,11 @@ __global__ __launch_bounds__(256) void latent_f32_kernel(Latent a) {
 
     while (pos < end) {
         const int b = seg;
-        const int span = uload(pl.prefix, b + 1) - uload(pl.prefix, b);
-        const int tiles = span - pl.seg_cost;
+        const int n = effective_keys(p, b), tiles = latent_tiles(n), span = tiles + pl.seg_cost;
         const int64_t left = end - pos;
         const int te = left < (int64_t)(span - tile) ? tile + (int)left : span;
         if (tile < tiles) {
             const int t1 = te < tiles ? te : tiles;
-            const int n = uload(pl.nkeys, b);
             const int lim = n - p.k + i;  // visible keys of the block
             const int64_t qrow = (((int64_t)b * (p.k + 1) + i) * p.Hq + h);
             f32x4_t q[QS];
@@ -188,66 +183,180 @@ __global__ __launch_bounds__(256) void latent_f32_kernel(Latent a) {
     }
 }
 
-// Merge of the partials of the sequences that several groups share.  One
-// workgroup per (group, row): the first group to start inside a sequence's tiles
-// merges it.  out = sum_i w_i o_i / sum_i w_i with w_i = 2^(lse_i - max).
-template <int DC>
-__global__ __launch_bounds__(256) void latent_combine_kernel(Latent a) {
-    constexpr int TPR = DC / 4, PG = 256 / TPR;  // threads a row, partials side by side
-    __shared__ float w[kCombineMaxWorkers];
-    __shared__ f32x4_t red[256];
-    const Problem &p = a.p;
+// ---- merge of the partials of the sequences that several groups share --------------
+// out = sum_i w_i o_i / sum_i w_i with w_i = 2^(lse_i - max).  A workgroup takes one
+// sequence (or, with more sequences than groups, the one that group g is the first
+// to start inside of).  What bounds it is the partials, written and read once: 67
+// MB for 256 groups of 128 rows of 512.
+struct Split {
+    int b, m;            // sequence, partials; m = 0: nothing to merge
+    int64_t start, wlo, T, workers;
+    bool sparse, tail0;  // a position per worker, some workers without; wlo's last segment, not its first
+    __device__ __forceinline__ int64_t slot(int x) const {
+        return sparse ? 2 * worker_of(start + x, T, workers) : 2 * (wlo + x) + (x == 0 && tail0 ? 1 : 0);
+    }
+};
+
+__device__ __forceinline__ Split split_of(const Latent &a, int block, bool per_group) {
     const Plan &pl = a.pl;
-    const int g = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+    Split s;
+    s.m = 0;
+    int tile0 = 1;
+    s.b = block;
+    if (per_group) {
+        s.b = pl.wstart[2 * block];
+        tile0 = pl.wstart[2 * block + 1];
+        if (s.b < 0) return s;
+    }
+    const int span = pl.prefix[s.b + 1] - pl.prefix[s.b], tiles = span - pl.seg_cost;
+    if (per_group && (tile0 == 0 || tile0 >= tiles)) return s;
+    s.T = pl.prefix[a.p.B];
+    s.start = pl.prefix[s.b];
+    s.workers = pl.workers;
+    s.wlo = worker_of(s.start, s.T, s.workers);
+    const int64_t whi = worker_of(s.start + tiles - 1, s.T, s.workers);
+    if (s.wlo == whi) return s;
+    if (per_group && worker_begin(block, s.T, s.workers) != worker_begin(s.wlo + 1, s.T, s.workers)) return s;
+    s.sparse = s.T < s.workers;
+    s.m = s.sparse ? tiles : (int)(whi - s.wlo + 1);
+    s.tail0 = !s.sparse && worker_begin(s.wlo, s.T, s.workers) < s.start;
+    return s;
+}
+
+// The query row of partial row `row`, or -1.
+__device__ __forceinline__ int64_t query_row(const Latent &a, int b, int row) {
     const int rb = row >> 4, i = rb / a.hb, h = 16 * (rb - i * a.hb) + (row & 15);
-    if (i > p.k || h >= p.Hq) return;
-    const int b = pl.wstart[2 * g], tile0 = pl.wstart[2 * g + 1];
-    if (b < 0) return;
-    const int span = pl.prefix[b + 1] - pl.prefix[b], tiles = span - pl.seg_cost;
-    if (tile0 == 0 || tile0 >= tiles) return;
-    const int64_t T = pl.prefix[p.B], start = pl.prefix[b];
-    const int64_t wlo = worker_of(start, T, pl.workers), whi = worker_of(start + tiles - 1, T, pl.workers);
-    if (wlo == whi || worker_begin(g, T, pl.workers) != worker_begin(wlo + 1, T, pl.workers)) return;
-    const bool sparse = T < pl.workers;  // a position per worker, some workers without
-    const int m = sparse ? tiles : (int)(whi - wlo + 1);
-    const bool tail0 = !sparse && worker_begin(wlo, T, pl.workers) < start;
-    auto slot = [&](int x) -> int64_t {
-        return sparse ? 2 * worker_of(start + x, T, pl.workers) : 2 * (wlo + x) + (x == 0 && tail0 ? 1 : 0);
-    };
-    float M = -INFINITY;
-    bool nan = false;
-    for (int x = tid; x < m; x += 256) w[x] = pl.part_lse[slot(x) * pl.rows + row];
-    __syncthreads();
-    for (int x = 0; x < m; ++x) {
-        const float v = w[x];
-        nan |= v != v;
-        M = fmaxf(M, v);
-    }
-    const float ref = M == -INFINITY ? 0.f : M;
-    __syncthreads();
-    for (int x = tid; x < m; x += 256) w[x] = exp2f(w[x] - ref);
-    __syncthreads();
-    float L = 0.f;
-    for (int x = 0; x < m; ++x) L += w[x];
-    if (nan) L = __builtin_nanf("");
-    const int pg = tid / TPR, d = 4 * (tid - pg * TPR);
-    f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    for (int x = pg; x < m; x += PG) {
-        const f32x4_t v = *reinterpret_cast<const f32x4_t *>(pl.part_o + (slot(x) * pl.rows + row) * DC + d);
-        const float wx = w[x];
-        if (wx != 0.f) acc += wx * v;
-    }
-    red[tid] = acc;
-    __syncthreads();
-    if (pg != 0) return;
-#pragma unroll
-    for (int x = 1; x < PG; ++x) acc += red[x * TPR + tid];
+    return i > a.p.k || h >= a.p.Hq ? -1 : ((int64_t)b * (a.p.k + 1) + i) * a.p.Hq + h;
+}
+
+// M: maximum of the log-sum-exps; L: sum of the weights (0: no visible key, NaN: a NaN partial).
+template <int DC>
+__device__ __forceinline__ void write_row(const Latent &a, int64_t qrow, int d, f32x4_t acc, float M, float L) {
+    const Problem &p = a.p;
     const float inv = L == 0.f ? 0.f : 1.f / L;
-    const int64_t qrow = ((int64_t)b * (p.k + 1) + i) * p.Hq + h;
     const float v[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
     if (p.out_dtype == SPIRE_F32) store_quad<4>(static_cast<uint8_t *>(p.out) + (qrow * DC + d) * 4, v, 1.f);
     else store_quad<2>(static_cast<uint8_t *>(p.out) + (qrow * DC + d) * 2, v, 1.f);
-    if (tid == 0 && p.lse != nullptr) p.lse[qrow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+    if (d == 0 && p.lse != nullptr) p.lse[qrow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
+}
+
+// Few partials a sequence: DC / 4 threads a row walk them, kRows rows a workgroup.
+constexpr int kCombineRows = 8;
+template <int DC>
+__global__ __launch_bounds__(256) void latent_combine_kernel(Latent a, int per_group) {
+    constexpr int TPR = DC / 4, AT = 256 / TPR;  // threads a row, rows at a time
+    const Plan &pl = a.pl;
+    const Split s = split_of(a, blockIdx.x, per_group != 0);
+    if (s.m == 0) return;
+    const int d = 4 * (threadIdx.x % TPR);
+    for (int row = blockIdx.y * kCombineRows + threadIdx.x / TPR; row < (int)(blockIdx.y + 1) * kCombineRows; row += AT) {
+        const int64_t qrow = query_row(a, s.b, row);
+        if (qrow < 0) continue;
+        // M: the largest log-sum-exp so far (-inf: none); sums are kept relative to it
+        float M = -INFINITY, L = 0.f;
+        f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int x0 = 0; x0 < s.m; x0 += 4) {
+            float lp[4];
+            f32x4_t o[4];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                lp[x] = -INFINITY;
+                if (x0 + x < s.m) {
+                    const int64_t at = s.slot(x0 + x) * pl.rows + row;
+                    lp[x] = pl.part_lse[at];
+                    o[x] = *reinterpret_cast<const f32x4_t *>(pl.part_o + at * DC + d);
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) top = fmaxf(top, lp[x]);
+            const float ref = top == -INFINITY ? 0.f : top, keep = M == -INFINITY ? 0.f : exp2f(M - ref);
+            M = top;
+            L *= keep;
+            acc *= keep;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+                const float w = lp[x] == -INFINITY ? 0.f : exp2f(lp[x] - ref);  // NaN: a NaN row
+                L += w;
+                if (w != 0.f) acc += w * o[x];
+            }
+        }
+        write_row<DC>(a, qrow, d, acc, M, L);
+    }
+}
+
+// Many partials a sequence (few sequences on all groups): a workgroup takes 64
+// dimensions of a row, 16 threads of 4 dimensions times 16 that share the partials.
+template <int DC>
+__global__ __launch_bounds__(256) void latent_combine_wide_kernel(Latent a) {
+    __shared__ float w[kCombineMaxWorkers];
+    __shared__ f32x4_t red[256];
+    __shared__ float stat[8];
+    const Plan &pl = a.pl;
+    const Split s = split_of(a, blockIdx.x, false);
+    const int row = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (s.m == 0) return;
+    const int64_t qrow = query_row(a, s.b, row);
+    if (qrow < 0) return;
+    const int col = tid & 15, pg = tid >> 4, d = 64 * blockIdx.z + 4 * col;
+    auto part = [&](int x) {
+        return *reinterpret_cast<const f32x4_t *>(pl.part_o + (s.slot(x) * pl.rows + row) * DC + d);
+    };
+    constexpr int U = 4;
+    f32x4_t o[U];
+#pragma unroll
+    for (int x = 0; x < U; ++x) o[x] = part(pg + 16 * x < s.m ? pg + 16 * x : 0);
+    float M = -INFINITY;
+    bool nan = false;
+    for (int x = tid; x < s.m; x += 256) {
+        const float v = pl.part_lse[s.slot(x) * pl.rows + row];
+        w[x] = v;
+        nan |= v != v;
+        M = fmaxf(M, v);
+    }
+#pragma unroll
+    for (int o2 = 32; o2 >= 1; o2 >>= 1) M = fmaxf(M, __shfl_xor(M, o2));
+    nan = __any(nan);
+    if (lane == 0) stat[wave] = nan ? __builtin_nanf("") : M;
+    __syncthreads();
+    M = -INFINITY;
+    nan = false;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        nan |= stat[x] != stat[x];
+        M = fmaxf(M, stat[x]);
+    }
+    const float ref = M == -INFINITY ? 0.f : M;
+    f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    float L = 0.f;
+    for (int x0 = pg; x0 < s.m; x0 += 16 * U) {
+#pragma unroll
+        for (int x = 0; x < U; ++x)
+            if (x0 + 16 * x < s.m) {
+                const float v = w[x0 + 16 * x], wx = v == -INFINITY ? 0.f : exp2f(v - ref);
+                L += wx;
+                if (wx != 0.f) acc += wx * o[x];
+            }
+#pragma unroll
+        for (int x = 0; x < U; ++x)
+            if (x0 + 16 * (U + x) < s.m) o[x] = part(x0 + 16 * (U + x));
+    }
+    red[tid] = acc;
+    __syncthreads();
+    // the first 16 threads: sums over the partials' threads, in a fixed order
+    if (pg == 0) {
+#pragma unroll
+        for (int x = 1; x < 16; ++x) acc += red[16 * x + col];
+    }
+    __syncthreads();
+    red[tid][0] = L;
+    __syncthreads();
+    if (pg != 0) return;
+    L = 0.f;
+#pragma unroll
+    for (int x = 0; x < 16; ++x) L += red[16 * x + col][0];
+    if (nan) L = __builtin_nanf("");
+    write_row<DC>(a, qrow, d, acc, M, L);
 }
 
 hipError_t launch_latent_f32(const Latent &a, hipStream_t st) {
@@ -257,11 +366,21 @@ hipError_t launch_latent_f32(const Latent &a, hipStream_t st) {
     return hipGetLastError();
 }
 
+// From 8 groups a sequence on, the partials are shared by threads (1 sequence of 65536
+// keys, 16 rows, 256 partials: WIDEUS us; one thread after the other FLATUS).
 hipError_t launch_latent_combine(const Latent &a, hipStream_t st) {
     if (a.pl.workers > kCombineMaxWorkers) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)a.pl.workers, (unsigned)a.pl.rows), block(256);
-    if (a.p.D == 512) hipLaunchKernelGGL(latent_combine_kernel<512>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(latent_combine_kernel<256>, grid, block, 0, st, a);
+    const bool big = a.p.D == 512;
+    if ((int64_t)a.p.B * 8 <= a.pl.workers) {
+        const dim3 grid((unsigned)a.p.B, (unsigned)a.pl.rows, (unsigned)(a.p.D / 64)), block(256);
+        if (big) hipLaunchKernelGGL(latent_combine_wide_kernel<512>, grid, block, 0, st, a);
+        else hipLaunchKernelGGL(latent_combine_wide_kernel<256>, grid, block, 0, st, a);
+        return hipGetLastError();
+    }
+    const int per_group = a.p.B > a.pl.workers;
+    const dim3 grid((unsigned)(per_group ? a.pl.workers : a.p.B), (unsigned)((a.pl.rows + kCombineRows - 1) / kCombineRows)), block(256);
+    if (big) hipLaunchKernelGGL(latent_combine_kernel<512>, grid, block, 0, st, a, per_group);
+    else hipLaunchKernelGGL(latent_combine_kernel<256>, grid, block, 0, st, a, per_group);
     return hipGetLastError();
 }
 

@@ -14,7 +14,7 @@
 // partials (normalised rows, base-2 log-sum-exp) that latent_combine merges.
 #pragma once
 
-#include "spire_internal.h"
+#include "mfma_common.h"
 
 namespace spire {
 
@@ -27,5 +27,33 @@ __device__ __forceinline__ void latent_place(const Latent &a, int &g, int &u) {
     g = lin / a.units;
     u = lin - g * a.units;
 }
+
+// Where group g starts and its positions: every workgroup forms the partition itself
+// (a launch of its own took 7 us), in LDS that is free again afterwards; the merge
+// finds the prefix sums and starts in the workspace.  False: nothing to do.
+template <int THREADS>
+__device__ __forceinline__ bool latent_start(const Latent &a, int g, int u, int32_t *lds, int &seg, int &tile,
+                                             int64_t &pos, int64_t &end) {
+    plan_in_kernel<THREADS>(a.p, a.pl, lds, lds + a.p.B + 1);
+    bool some = false;
+    if (g < a.pl.workers) {
+        const int64_t T = __builtin_amdgcn_readfirstlane(lds[a.p.B]);
+        pos = worker_begin(g, T, a.pl.workers);
+        end = worker_begin(g + 1, T, a.pl.workers);
+        some = pos < end;
+        if (some) locate(lds, a.p.B, 1, pos, seg, tile);
+        if (u == 0 && threadIdx.x == 0) {
+            a.pl.wstart[2 * g] = some ? seg : -1;
+            a.pl.wstart[2 * g + 1] = some ? tile : 0;
+        }
+    }
+    seg = __builtin_amdgcn_readfirstlane(seg);
+    tile = __builtin_amdgcn_readfirstlane(tile);
+    __syncthreads();
+    return some;
+}
+
+// Positions of sequence b: its tiles and the phantoms of its segment.
+__device__ __forceinline__ int latent_tiles(int n) { return n > 0 ? (n + kLatentTile - 1) / kLatentTile : 1; }
 
 }  // namespace spire

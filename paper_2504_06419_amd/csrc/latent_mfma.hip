@@ -160,12 +160,9 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
     const Plan &pl = a.pl;
     int g, u;
     latent_place(a, g, u);
-    if (g >= pl.workers) return;
-    const int64_t T = (int64_t)uload(pl.prefix, p.B);
-    int64_t pos = worker_begin(g, T, pl.workers);
-    const int64_t end = worker_begin(g + 1, T, pl.workers);
-    if (pos >= end) return;
-    int seg = uload(pl.wstart, 2 * g), tile = uload(pl.wstart, 2 * g + 1);
+    int64_t pos = 0, end = 0;
+    int seg = 0, tile = 0;
+    if (!latent_start<512>(a, g, u, reinterpret_cast<int32_t *>(smem), seg, tile, pos, end)) return;
     const int64_t begin = pos;
     float sc = p.sm_scale_log2, vscale = 1.f;
     if (FP8) {
@@ -194,8 +191,7 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
 
     while (pos < end) {
         const int b = seg;
-        const int span = uload(pl.prefix, b + 1) - uload(pl.prefix, b);
-        const int tiles = span - pl.seg_cost;
+        const int n = effective_keys(p, b), tiles = latent_tiles(n), span = tiles + pl.seg_cost;
         const int64_t left = end - pos;
         const int te = left < (int64_t)(span - tile) ? tile + (int)left : span;
         if (tile >= tiles) {  // phantom positions only
@@ -205,7 +201,6 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
             continue;
         }
         const int t1 = te < tiles ? te : tiles;
-        const int n = uload(pl.nkeys, b);
         // keys that block x of the unit sees; the first block sees the fewest
         auto limit = [&](int x) {
             cLatent *A = arguments();

@@ -1134,9 +1134,7 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
     pl.part_lse = reinterpret_cast<float *>(ws + L.part_lse);
     pl.part_o = reinterpret_cast<float *>(ws + L.part_o);
     Recorder rec(opts);
-    hipError_t e = rec.run(KID_PLAN, stream, launch_plan, p, pl);
-    if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "plan launch: %s", hipGetErrorString(e));
-    e = rec.run(KID_LATENT, stream, [&] { return matrix ? launch_latent_mfma(a, stream) : launch_latent_f32(a, stream); });
+    hipError_t e = rec.run(KID_LATENT, stream, [&] { return matrix ? launch_latent_mfma(a, stream) : launch_latent_f32(a, stream); });
     if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "latent attention launch: %s", hipGetErrorString(e));
     e = rec.run(KID_LATENT_COMBINE, stream, [&] { return launch_latent_combine(a, stream); });
     if (e != hipSuccess) return fail(SPIRE_ERR_HIP, "latent combine launch: %s", hipGetErrorString(e));
