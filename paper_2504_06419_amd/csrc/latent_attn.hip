@@ -367,7 +367,7 @@ hipError_t launch_latent_f32(const Latent &a, hipStream_t st) {
 }
 
 // From 8 groups a sequence on, the partials are shared by threads (1 sequence of 65536
-// keys, 16 rows, 256 partials: WIDEUS us; one thread after the other FLATUS).
+// keys, 16 rows, 256 partials: 10 us; one thread after the other 71).
 hipError_t launch_latent_combine(const Latent &a, hipStream_t st) {
     if (a.pl.workers > kCombineMaxWorkers) return hipErrorInvalidValue;
     const bool big = a.p.D == 512;
