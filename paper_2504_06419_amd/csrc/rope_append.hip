@@ -9,6 +9,8 @@
 // The angle is a product in fp64, reduced to a fraction of a turn there (a far
 // position times a frequency has more bits than fp32 holds: at position 10^6 an
 // fp32 angle is off by 0.03), its sine and cosine are fp32.
+#include <type_traits>
+
 #include "convert.h"
 
 namespace spire {
@@ -156,208 +158,241 @@ __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendArgs a) 
 
 // ---- rows of 8-element items (vector paths) ---------------------------------------
 //
-// One workgroup takes a few tokens, every row of them.  The sines and cosines of a
-// token are formed once, by the first threads, and stand in LDS for all its heads
-// (fp64 products per head would cost more than the memory traffic).  A row is D / 8
-// items, one per lane; item i holds two quads of elements: its 4 pairs' first and
-// second halves (4 i and 4 i + rot / 2) or 4 neighbouring pairs, so a rotation stays
-// in its lane.  D / 8 is a power of two up to 64: a norm's sum is a few shuffles.
-// Bound by memory for prompts, by the chain position -> angle -> row for few tokens.
-struct Quads {
-    float a[4], b[4];
+// A row is D / 8 items, one per lane; item i holds two quads of elements: its 4 pairs'
+// first and second halves (4 i and 4 i + rot / 2) or 4 neighbouring pairs, so that a
+// rotation stays in its lane.  D / 8 is a power of two up to 64: a norm's sum is a few
+// shuffles.  A wave takes some heads of one token, 512 / D of them a round.  A lane
+// keeps its place i over the rounds, and with it its 4 sines and cosines (formed once
+// a wave, one pair per lane, and passed through LDS) and its norm weights: with the
+// angles formed per head the instructions, not the memory, set the time.  The next
+// round's loads are on their way while a round is computed.
+constexpr int kWaves = 4;         // of a workgroup
+constexpr int kMaxPairs = 256;    // of a rotation: D <= 512
+
+template <int ES>
+struct Quads {  // as loaded: bf16 or fp32
+    using V = typename std::conditional<ES == 4, uint4, uint2>::type;
+    V a, b;
+    __device__ __forceinline__ void load(const void *row, int oa, int ob) {
+        a = *reinterpret_cast<const V *>(static_cast<const uint8_t *>(row) + oa * ES);
+        b = *reinterpret_cast<const V *>(static_cast<const uint8_t *>(row) + ob * ES);
+    }
+    static __device__ __forceinline__ void floats(const V &v, float *x) {
+        if constexpr (ES == 4) {
+            x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y);
+            x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
+        } else {
+            x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+            x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+        }
+    }
+    __device__ __forceinline__ void floats(float x[8]) const {
+        floats(a, x);
+        floats(b, x + 4);
+    }
 };
 
-__device__ __forceinline__ void quad_places(int i, int rot, bool interleaved, int &oa, int &ob) {
+__device__ __forceinline__ void item_places(int i, int rot, bool interleaved, int &oa, int &ob) {
     const bool halves = 8 * i < rot && !interleaved;
     oa = halves ? 4 * i : 8 * i;
     ob = halves ? 4 * i + (rot >> 1) : 8 * i + 4;
 }
 
-// `tab`: (cos, sin) of the token's pairs.
-__device__ __forceinline__ void rotate_item(Quads &x, int i, const RopeDev &r, int rot, const float2 *tab) {
-    if (8 * i >= rot) return;
-    float2 t[4];
+__device__ __forceinline__ void rotate_pair(float &u, float &v, float2 cs) {
+    const float p = u * cs.x - v * cs.y, q = v * cs.x + u * cs.y;
+    u = p;
+    v = q;
+}
+
+// `cs`: (cos, sin) of the item's 4 pairs; x: quad a, then quad b
+__device__ __forceinline__ void rotate_item(float x[8], bool interleaved, const float2 cs[4]) {
+    if (interleaved) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) t[e] = tab[4 * i + e];
-    auto turn2 = [](float &u, float &v, float2 cs) {
-        const float p = u * cs.x - v * cs.y, q = v * cs.x + u * cs.y;
-        u = p;
-        v = q;
-    };
-    if (r.interleaved) {
-        turn2(x.a[0], x.a[1], t[0]);
-        turn2(x.a[2], x.a[3], t[1]);
-        turn2(x.b[0], x.b[1], t[2]);
-        turn2(x.b[2], x.b[3], t[3]);
+        for (int e = 0; e < 4; ++e) rotate_pair(x[2 * e], x[2 * e + 1], cs[e]);
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) turn2(x.a[e], x.b[e], t[e]);
+        for (int e = 0; e < 4; ++e) rotate_pair(x[e], x[4 + e], cs[e]);
     }
 }
 
-// x / sqrt(mean(x^2) + eps) * w over the `lanes` lanes (a power of two) that hold the row.
-__device__ __forceinline__ void norm_item(Quads &x, const float *w, int oa, int ob, int D, int lanes, float eps) {
+// x / sqrt(mean(x^2) + eps) * w over the 1 << shift lanes that hold the row
+__device__ __forceinline__ void norm_item(float x[8], const float w[8], int shift, float eps) {
     float ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) ss = fmaf(x.a[e], x.a[e], fmaf(x.b[e], x.b[e], ss));
-    for (int o = lanes >> 1; o >= 1; o >>= 1) ss += __shfl_xor(ss, o);
-    const float r = 1.f / sqrtf(ss / (float)D + eps);
-    const float4 wa = *reinterpret_cast<const float4 *>(w + oa), wb = *reinterpret_cast<const float4 *>(w + ob);
-    x.a[0] *= r * wa.x; x.a[1] *= r * wa.y; x.a[2] *= r * wa.z; x.a[3] *= r * wa.w;
-    x.b[0] *= r * wb.x; x.b[1] *= r * wb.y; x.b[2] *= r * wb.z; x.b[3] *= r * wb.w;
+    for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+#pragma unroll
+    for (int b = 5; b >= 0; --b)
+        if (b < shift) ss += __shfl_xor(ss, 1 << b);
+    const float r = 1.f / sqrtf(ss / (float)(8 << shift) + eps);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] *= r * w[e];
 }
 
-__device__ __forceinline__ void store_item(uint8_t *row, int es, const Quads &x, int oa, int ob, float scale) {
-    if (es == 4) {
-        store_quad<4>(row + 4 * oa, x.a, 1.f);
-        store_quad<4>(row + 4 * ob, x.b, 1.f);
-    } else if (es == 2) {
-        store_quad<2>(row + 2 * oa, x.a, 1.f);
-        store_quad<2>(row + 2 * ob, x.b, 1.f);
+__device__ __forceinline__ void load_weights(const float *w, int oa, int ob, float x[8]) {
+    if (w == nullptr) return;
+    const float4 a = *reinterpret_cast<const float4 *>(w + oa), b = *reinterpret_cast<const float4 *>(w + ob);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+
+// two fp32 -> bf16, nearest even (the conversion instruction)
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
+    const pair p = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, p);
+}
+
+__device__ __forceinline__ void store_item(uint8_t *row, int es, const float x[8], int oa, int ob, float scale) {
+    if (es == 2) {
+        *reinterpret_cast<uint2 *>(row + 2 * oa) = make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
+        *reinterpret_cast<uint2 *>(row + 2 * ob) = make_uint2(bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+    } else if (es == 4) {
+        store_quad<4>(row + 4 * oa, x, 1.f);
+        store_quad<4>(row + 4 * ob, x + 4, 1.f);
     } else {
-        store_quad<1>(row + oa, x.a, scale);
-        store_quad<1>(row + ob, x.b, scale);
+        store_quad<1>(row + oa, x, scale);
+        store_quad<1>(row + ob, x + 4, scale);
     }
 }
 
-constexpr int kVecThreads = 256;
-constexpr int kVecPairs = 512;  // (cos, sin) pairs a workgroup holds
-
-__device__ __forceinline__ void angles_to_lds(const RopeDev &rope, int t0, int tokens, float2 *tab) {
+// The token's (cos, sin) of item i's pairs, through this wave's part of LDS.
+__device__ __forceinline__ void item_angles(const RopeDev &rope, int t, int i, int lane, float2 *tab, float2 cs[4]) {
     const int half = rope.rot >> 1;
-    for (int x = threadIdx.x; x < tokens * half; x += kVecThreads) {
-        const int t = x / half;
+    for (int x = lane; x < half; x += 64) {
         float c, s;
-        angle(rope, t0 + t, x - t * half, c, s);
+        angle(rope, t, x, c, s);
         tab[x] = make_float2(c, s);
     }
+    // one wave's LDS accesses keep their order; the compiler has to keep it too
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (8 * i < rope.rot)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cs[e] = tab[4 * i + e];
 }
 
-__global__ __launch_bounds__(kVecThreads) void qkv_append_vec_kernel(QkvArgs a, int per, int shift) {
-    __shared__ float2 tab[kVecPairs];
-    const int t0 = blockIdx.x * per, tokens = a.N - t0 < per ? a.N - t0 : per;
-    const int heads = a.Hq + 2 * a.Hkv, items = tokens * heads << shift;  // D / 8 = 1 << shift items a row
-    const int i = threadIdx.x & ((1 << shift) - 1);
-    struct Where {
-        const void *src;
-        int64_t at;
-        int t, h, rot, oa, ob;
+// By value: a choice between variables becomes one between their addresses, and those then live in scratch memory.
+template <class T>
+__device__ __forceinline__ T pick(bool first, T a, T b) {
+    return first ? a : b;
+}
+
+// slices: waves a token; rounds: rounds a wave.
+template <int ES>
+__global__ __launch_bounds__(64 * kWaves) void qkv_append_vec_kernel(QkvArgs a, int slices, int rounds, int shift) {
+    __shared__ float2 tab[kWaves][kMaxPairs];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int job = blockIdx.x * kWaves + wave, t = job / slices;
+    if (t >= a.N) return;  // no barrier of the workgroup follows
+    const int R = 64 >> shift, i = lane & ((1 << shift) - 1), es = a.kv.elem;
+    const int heads = a.Hq + 2 * a.Hkv, h0 = (job - t * slices) * rounds * R;
+    const int end = heads - h0 < rounds * R ? heads : h0 + rounds * R;
+    const bool inter = a.rope.interleaved != 0;
+    const uint8_t *qb = static_cast<const uint8_t *>(a.q) + t * a.q_stride * ES;
+    const uint8_t *kb = static_cast<const uint8_t *>(a.k) + (t * a.k_stride - (int64_t)a.Hq * a.D) * ES;
+    const uint8_t *vb = static_cast<const uint8_t *>(a.v) + (t * a.v_stride - (int64_t)(a.Hq + a.Hkv) * a.D) * ES;
+    int oa, ob;
+    item_places(i, a.rope.rot, inter, oa, ob);
+    auto load = [&](int h, Quads<ES> &x) {
+        if (h >= end) h = end - 1;  // loaded, not used
+        const bool val = h >= a.Hq + a.Hkv;
+        const uint8_t *b = pick(h < a.Hq, qb, pick(val, vb, kb));
+        x.load(b + (int64_t)h * a.D * ES, val ? 8 * i : oa, val ? 8 * i + 4 : ob);
     };
-    auto where = [&](int x) {
-        Where w;
-        const int row = x >> shift;
-        w.t = tokens == 1 ? 0 : row / heads;
-        w.h = row - w.t * heads;
-        const int64_t tok = t0 + w.t;
-        const bool q = w.h < a.Hq, val = w.h >= a.Hq + a.Hkv;
-        w.src = q ? a.q : (val ? a.v : a.k);
-        w.at = tok * (q ? a.q_stride : (val ? a.v_stride : a.k_stride)) +
-               (int64_t)(w.h - (q ? 0 : (val ? a.Hq + a.Hkv : a.Hq))) * a.D;
-        w.rot = val ? 0 : a.rope.rot;
-        quad_places(i, w.rot, a.rope.interleaved != 0, w.oa, w.ob);
-        return w;
-    };
-    auto load = [&](const Where &w) {
-        Quads x;
-        load_quad(w.src, a.in_dtype, w.at + w.oa, x.a);
-        load_quad(w.src, a.in_dtype, w.at + w.ob, x.b);
-        return x;
-    };
-    Where w;
-    Quads x;
-    if ((int)threadIdx.x < items) {  // on its way while the angles are formed
-        w = where(threadIdx.x);
-        x = load(w);
-    }
-    angles_to_lds(a.rope, t0, tokens, tab);
-    __syncthreads();
-    for (int y = threadIdx.x; y < items; y += kVecThreads) {
-        Where wn;
-        Quads xn;
-        if (y + kVecThreads < items) {
-            wn = where(y + kVecThreads);
-            xn = load(wn);
+    int h = h0 + (lane >> shift);
+    Quads<ES> now, next;
+    load(h, now);
+    const int64_t slot = a.slots[t];
+    float qw[8], kw[8];
+    load_weights(a.qw, oa, ob, qw);
+    load_weights(a.kw, oa, ob, kw);
+    float2 cs[4];
+    if (h0 < a.Hq + a.Hkv) item_angles(a.rope, t, i, lane, tab[wave], cs);
+    const int64_t at = slot_row(slot, a.rpb, a.kv.num_blocks, a.kv.s_blk, a.kv.s_tok);
+    uint8_t *const qo = static_cast<uint8_t *>(a.q_out) + (int64_t)t * a.Hq * a.D * a.out_es;
+    uint8_t *const ko = const_cast<uint8_t *>(a.kv.k) + at * es, *const vo = const_cast<uint8_t *>(a.kv.v) + at * es;
+    const float *const k_scale = a.kv.k_scale, *const v_scale = a.kv.v_scale;
+    for (int n = 0; n < rounds; ++n, h += R) {
+        if (n + 1 < rounds) load(h + R, next);
+        if (h < end) {
+            float x[8];
+            now.floats(x);
+            const bool q = h < a.Hq, val = h >= a.Hq + a.Hkv;
+            if (q ? a.qw != nullptr : (!val && a.kw != nullptr)) {
+                float w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e] = pick(q, qw[e], kw[e]);
+                norm_item(x, w, shift, a.eps);
+            }
+            if (!val && 8 * i < a.rope.rot) rotate_item(x, inter, cs);
+            const int g = h - a.Hq - (val ? a.Hkv : 0);
+            uint8_t *to = q ? qo + (int64_t)h * a.D * a.out_es : pick(val, vo, ko) + g * a.kv.s_head * es;
+            if (q || at >= 0)
+                store_item(to, pick(q, a.out_es, es), x, val ? 8 * i : oa, val ? 8 * i + 4 : ob,
+                           q || es != 1 ? 1.f : pick(val, v_scale, k_scale)[g]);
         }
-        const bool q = w.h < a.Hq, val = w.h >= a.Hq + a.Hkv;
-        const float *weight = q ? a.qw : (val ? nullptr : a.kw);
-        if (weight != nullptr) norm_item(x, weight, w.oa, w.ob, a.D, 1 << shift, a.eps);
-        rotate_item(x, i, a.rope, w.rot, tab + w.t * (a.rope.rot >> 1));
-        if (q) {
-            store_item(static_cast<uint8_t *>(a.q_out) + ((int64_t)(t0 + w.t) * a.Hq + w.h) * a.D * a.out_es, a.out_es, x,
-                       w.oa, w.ob, 1.f);
-        } else {
-            const int g = w.h - a.Hq - (val ? a.Hkv : 0), es = a.kv.elem;
-            const int64_t at = slot_row(a.slots[t0 + w.t], a.rpb, a.kv.num_blocks, a.kv.s_blk, a.kv.s_tok);
-            if (at >= 0)
-                store_item(const_cast<uint8_t *>(val ? a.kv.v : a.kv.k) + (at + g * a.kv.s_head) * es, es, x, w.oa, w.ob,
-                           es == 1 ? (val ? a.kv.v_scale : a.kv.k_scale)[g] : 1.f);
-        }
-        w = wn;
-        x = xn;
+        now = next;
     }
 }
 
-// The tokens' latents come first, 1 << shift items each, so that none crosses a
-// wave; then rows of 1 << rshift items: a token's key part and its queries' parts.
-__global__ __launch_bounds__(kVecThreads) void latent_append_vec_kernel(LatentAppendArgs a, int per, int shift, int rshift) {
-    __shared__ float2 tab[kVecPairs];
-    const int t0 = blockIdx.x * per, tokens = a.N - t0 < per ? a.N - t0 : per;
-    const int lat = tokens << shift, items = lat + (tokens * (1 + a.Hq) << rshift);
-    struct Where {
-        const void *src;
-        int64_t at;
-        int t, h, i, rot, oa, ob;  // h: -2 the latent, -1 the key part
+// The first `groups` workgroups take the latents, 512 / Dc tokens a wave, the others the
+// key parts and the queries' parts.
+template <int ES>
+__global__ __launch_bounds__(64 * kWaves) void latent_append_vec_kernel(LatentAppendArgs a, int groups, int shift,
+                                                                        int slices, int rounds, int rshift) {
+    __shared__ float2 tab[kWaves][kMaxPairs];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int es = a.kv.elem;
+    auto cache = [&](int64_t slot, int d) {
+        const int64_t at = slot_row(slot, a.rpb, a.kv.num_blocks, a.kv.s_blk, a.kv.s_tok);
+        return at < 0 ? nullptr : const_cast<uint8_t *>(a.kv.k) + (at + d) * es;
     };
-    auto where = [&](int x) {
-        Where w;
-        const bool c = x < lat;
-        const int row = (x - lat) >> rshift;
-        w.t = c ? x >> shift : (tokens == 1 ? 0 : row / (1 + a.Hq));
-        w.h = c ? -2 : row - w.t * (1 + a.Hq) - 1;
-        w.i = c ? x & ((1 << shift) - 1) : (x - lat) & ((1 << rshift) - 1);
-        const int64_t tok = t0 + w.t;
-        w.src = c ? a.c : (w.h < 0 ? a.k : a.q);
-        w.at = c ? tok * a.c_stride : (w.h < 0 ? tok * a.k_stride : tok * a.q_stride + w.h * a.q_head_stride);
-        w.rot = c ? 0 : a.rope.rot;
-        quad_places(w.i, w.rot, a.rope.interleaved != 0, w.oa, w.ob);
-        return w;
-    };
-    auto load = [&](const Where &w) {
-        Quads x;
-        load_quad(w.src, a.in_dtype, w.at + w.oa, x.a);
-        load_quad(w.src, a.in_dtype, w.at + w.ob, x.b);
-        return x;
-    };
-    Where w;
-    Quads x;
-    if ((int)threadIdx.x < items) {
-        w = where(threadIdx.x);
-        x = load(w);
+    const float scale = es == 1 ? a.kv.k_scale[0] : 1.f;
+    Quads<ES> now, next;
+    float x[8];
+    if ((int)blockIdx.x < groups) {
+        const int i = lane & ((1 << shift) - 1);
+        const int t = (blockIdx.x * kWaves + wave) * (64 >> shift) + (lane >> shift);
+        if (t >= a.N) return;  // whole rows: the norm's lanes stay together
+        now.load(static_cast<const uint8_t *>(a.c) + t * a.c_stride * ES, 8 * i, 8 * i + 4);
+        const int64_t slot = a.slots[t];
+        float w[8];
+        load_weights(a.w, 8 * i, 8 * i + 4, w);
+        uint8_t *to = cache(slot, 0);
+        now.floats(x);
+        if (a.w != nullptr) norm_item(x, w, shift, a.eps);
+        if (to != nullptr) store_item(to, es, x, 8 * i, 8 * i + 4, scale);
+        return;
     }
-    angles_to_lds(a.rope, t0, tokens, tab);
-    __syncthreads();
-    for (int y = threadIdx.x; y < items; y += kVecThreads) {
-        Where wn;
-        Quads xn;
-        if (y + kVecThreads < items) {
-            wn = where(y + kVecThreads);
-            xn = load(wn);
+    const int job = (blockIdx.x - groups) * kWaves + wave, t = job / slices;
+    if (t >= a.N) return;
+    const int R = 64 >> rshift, i = lane & ((1 << rshift) - 1);
+    const int h0 = (job - t * slices) * rounds * R, end = a.Hq + 1 - h0 < rounds * R ? a.Hq + 1 : h0 + rounds * R;
+    const bool inter = a.rope.interleaved != 0;
+    const uint8_t *kb = static_cast<const uint8_t *>(a.k) + t * a.k_stride * ES;
+    const uint8_t *qb = static_cast<const uint8_t *>(a.q) + (t * a.q_stride - a.q_head_stride) * ES;
+    int oa, ob;
+    item_places(i, a.rope.rot, inter, oa, ob);
+    auto load = [&](int h, Quads<ES> &y) {  // row 0: the key part
+        if (h >= end) h = end - 1;
+        y.load(h == 0 ? kb : qb + h * a.q_head_stride * ES, oa, ob);
+    };
+    int h = h0 + (lane >> rshift);
+    load(h, now);
+    const int64_t slot = a.slots[t];
+    float2 cs[4];
+    item_angles(a.rope, t, i, lane, tab[wave], cs);
+    uint8_t *const to = cache(slot, a.Dc);
+    const int64_t q_row = (int64_t)(a.Dc + a.Dr) * a.out_es;
+    uint8_t *const qo = static_cast<uint8_t *>(a.q_out) + ((int64_t)t * a.Hq - 1) * q_row + (int64_t)a.Dc * a.out_es;
+    for (int n = 0; n < rounds; ++n, h += R) {
+        if (n + 1 < rounds) load(h + R, next);
+        if (h < end) {
+            now.floats(x);
+            if (8 * i < a.rope.rot) rotate_item(x, inter, cs);
+            if (h > 0 || to != nullptr) store_item(h > 0 ? qo + h * q_row : to, h > 0 ? a.out_es : es, x, oa, ob, scale);
         }
-        if (a.w != nullptr && w.h == -2) norm_item(x, a.w, w.oa, w.ob, a.Dc, 1 << shift, a.eps);
-        rotate_item(x, w.i, a.rope, w.rot, tab + w.t * (a.rope.rot >> 1));
-        if (w.h >= 0) {
-            store_item(static_cast<uint8_t *>(a.q_out) +
-                           (((int64_t)(t0 + w.t) * a.Hq + w.h) * (a.Dc + a.Dr) + a.Dc) * a.out_es,
-                       a.out_es, x, w.oa, w.ob, 1.f);
-        } else {
-            const int es = a.kv.elem;
-            const int64_t at = slot_row(a.slots[t0 + w.t], a.rpb, a.kv.num_blocks, a.kv.s_blk, a.kv.s_tok);
-            if (at >= 0)
-                store_item(const_cast<uint8_t *>(a.kv.k) + (at + (w.h == -1 ? a.Dc : 0)) * es, es, x, w.oa, w.ob,
-                           es == 1 ? a.kv.k_scale[0] : 1.f);
-        }
-        w = wn;
-        x = xn;
+        now = next;
     }
 }
 
@@ -383,15 +418,19 @@ static bool on_quads(const void *p, int es, int64_t s0 = 0, int64_t s1 = 0, int6
     return (uintptr_t)p % (4 * es) == 0 && s0 % 4 == 0 && s1 % 4 == 0 && s2 % 4 == 0;
 }
 
-static bool rope_on_items(const RopeDev &r, int D) { return r.rot % 8 == 0 && r.rot <= D && r.rot / 2 <= kVecPairs; }
+// at most 256 pairs: D <= 512
+static bool rope_on_items(const RopeDev &r) { return r.rot % 8 == 0; }
 
-// Tokens a workgroup: enough items for its threads, where that leaves workgroups
-// for every CU twice over; and the angles' place.
-static int tokens_per_group(int N, int items, int rot) {
-    int per = items >= kVecThreads ? 1 : kVecThreads / items;
-    if (rot > 0 && per > kVecPairs / (rot / 2)) per = kVecPairs / (rot / 2);
-    if (per > (N + 511) / 512) per = (N + 511) / 512;
-    return per < 1 ? 1 : per;
+// a wave's number is 32-bit
+static bool in_int(int64_t N, int64_t heads) { return N * heads <= INT32_MAX - 65536; }
+
+// Rounds a wave, of the `all` rounds of a token.  Several once every SIMD has 4 waves (at
+// 1024 tokens, 32 + 2 x 8 heads of 128, bf16: 1 round a wave 14.0 us, 3 rounds 12.7); at
+// most 6, where the angles no longer cost and shorter waves balance better (at 8192
+// tokens: 12 rounds 51.7 us, 6 rounds 47.3).
+static int rounds_per_wave(int64_t N, int all) {
+    const int64_t n = N * all / 4096, most = n < 1 ? 1 : (n > 6 ? 6 : n), slices = (all + most - 1) / most;
+    return (int)((all + slices - 1) / slices);
 }
 
 hipError_t launch_qkv_append(const QkvAppend &x, hipStream_t st) {
@@ -399,11 +438,14 @@ hipError_t launch_qkv_append(const QkvAppend &x, hipStream_t st) {
               x.kv, x.slots, x.q_out, x.eps, x.in_dtype, x.out_dtype == SPIRE_F32 ? 4 : 2, x.N, x.Hq, x.Hkv, x.D,
               x.kv.page_size > 0 ? x.kv.page_size : x.kv.capacity};
     const int shift = item_shift(x.D), ies = x.in_dtype == SPIRE_F32 ? 4 : 2, es = x.kv.elem;
-    if (shift >= 0 && rope_on_items(a.rope, x.D) && on_quads(x.q, ies, x.q_stride) && on_quads(x.k, ies, x.k_stride) &&
+    if (shift >= 0 && in_int(x.N, x.Hq + 2 * x.Hkv) && rope_on_items(a.rope) && on_quads(x.q, ies, x.q_stride) && on_quads(x.k, ies, x.k_stride) &&
         on_quads(x.v, ies, x.v_stride) && on_quads(x.q_out, a.out_es) && on_quads(x.q_weight, 4) && on_quads(x.k_weight, 4) &&
         on_quads(x.kv.k, es, x.kv.s_blk, x.kv.s_head, x.kv.s_tok) && on_quads(x.kv.v, es)) {
-        const int per = tokens_per_group(x.N, (x.Hq + 2 * x.Hkv) << shift, a.rope.rot);
-        hipLaunchKernelGGL(qkv_append_vec_kernel, dim3((unsigned)((x.N + (int64_t)per - 1) / per)), dim3(kVecThreads), 0, st, a, per, shift);
+        const int R = 64 >> shift, all = (x.Hq + 2 * x.Hkv + R - 1) / R, rounds = rounds_per_wave(x.N, all);
+        const int slices = (all + rounds - 1) / rounds;
+        const dim3 grid((unsigned)(((int64_t)x.N * slices + kWaves - 1) / kWaves)), block(64 * kWaves);
+        if (ies == 4) hipLaunchKernelGGL(qkv_append_vec_kernel<4>, grid, block, 0, st, a, slices, rounds, shift);
+        else hipLaunchKernelGGL(qkv_append_vec_kernel<2>, grid, block, 0, st, a, slices, rounds, shift);
         return hipGetLastError();
     }
     const int64_t rows = (int64_t)x.N * (x.Hq + 2 * x.Hkv);
@@ -417,11 +459,15 @@ hipError_t launch_latent_append(const LatentAppend &x, hipStream_t st) {
                        x.out_dtype == SPIRE_F32 ? 4 : 2, x.N, x.Hq, x.Dc, x.Dr,
                        x.kv.page_size > 0 ? x.kv.page_size : x.kv.capacity};
     const int shift = item_shift(x.Dc), rshift = item_shift(x.Dr), ies = x.in_dtype == SPIRE_F32 ? 4 : 2, es = x.kv.elem;
-    if (shift >= 0 && rshift >= 0 && rope_on_items(a.rope, x.Dr) && on_quads(x.c, ies, x.c_stride) &&
+    if (shift >= 0 && rshift >= 0 && in_int(x.N, 1 + x.Hq) && rope_on_items(a.rope) && on_quads(x.c, ies, x.c_stride) &&
         on_quads(x.k, ies, x.k_stride) && on_quads(x.q, ies, x.q_stride, x.q_head_stride) && on_quads(x.q_out, a.out_es) &&
         on_quads(x.weight, 4) && on_quads(x.kv.k, es, x.kv.s_blk, x.kv.s_tok)) {
-        const int per = tokens_per_group(x.N, (1 << shift) + ((1 + x.Hq) << rshift), a.rope.rot);
-        hipLaunchKernelGGL(latent_append_vec_kernel, dim3((unsigned)((x.N + (int64_t)per - 1) / per)), dim3(kVecThreads), 0, st, a, per, shift, rshift);
+        const int R = 64 >> rshift, all = (1 + x.Hq + R - 1) / R, rounds = rounds_per_wave(x.N, all);
+        const int slices = (all + rounds - 1) / rounds, per = kWaves * (64 >> shift);
+        const int groups = (int)(((int64_t)x.N + per - 1) / per);
+        const dim3 grid((unsigned)(groups + ((int64_t)x.N * slices + kWaves - 1) / kWaves)), block(64 * kWaves);
+        if (ies == 4) hipLaunchKernelGGL(latent_append_vec_kernel<4>, grid, block, 0, st, a, groups, shift, slices, rounds, rshift);
+        else hipLaunchKernelGGL(latent_append_vec_kernel<2>, grid, block, 0, st, a, groups, shift, slices, rounds, rshift);
         return hipGetLastError();
     }
     const int64_t rows = (int64_t)x.N * (x.Hq + 2);
