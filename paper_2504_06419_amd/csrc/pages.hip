@@ -7,12 +7,20 @@
 //
 // Both are a prefix sum over the sequences (one workgroup: B <= 8192) followed by
 // a flat pass over tokens and pages, each of which finds its sequence by bisection
-// in the prefix sums.  All of it is integer arithmetic in a fixed order.
+// in the prefix sums.  All of it is integer arithmetic in a fixed order.  Lengths may
+// be updated in place, so no second workgroup can form the sums for itself: the flat
+// pass is a launch of its own, or the same workgroup's where the tokens are few.
+// Bound by latency (a chain of dependent loads, and the launches), not by bytes.
 #include "spire_internal.h"
 
 namespace spire {
 
 constexpr int kPageThreads = 1024;
+constexpr int kPagePer = 8;        // sequences a thread: B <= 8192
+constexpr int kOneLaunchB = 1024;  // sequences whose sums stand in LDS
+// Tokens up to which the flat pass is the scanning workgroup's own (256 sequences, 2048
+// tokens: 7.7 us, two launches 10.4; 4096 tokens: 9.9 and 9.4).
+constexpr int kOneLaunchTokens = 2048;
 constexpr int kFillThreads = 256;
 constexpr int kFillTokens = 4;  // consecutive tokens per thread
 
@@ -21,7 +29,7 @@ struct PageState {
     int32_t *head;    // [0]: free pages before, [1]: pages handed out or pushed
     int32_t *first;   // pages of the sequences before b
     int32_t *len;     // lengths before (extend), first column pushed (release)
-    int32_t *given;   // pages of b; -1: refused
+    int32_t *given;   // pages of b; -1: refused (extend)
 };
 
 __host__ __device__ __forceinline__ PageState page_state(void *ws, int B) {
@@ -30,30 +38,55 @@ __host__ __device__ __forceinline__ PageState page_state(void *ws, int B) {
     return PageState{w, w + 64, w + 64 + n, w + 64 + 2 * n};
 }
 
-// Exclusive prefix sum over the workgroup's threads; `total` is the whole sum.
-__device__ __forceinline__ int64_t scan_block(int64_t x, int64_t *sums, int64_t &total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t incl = x;
+// Exclusive prefix sums of two counts over the workgroup's threads, x and y left as
+// the sums before the thread, the whole sums in all_x and all_y.
+struct ScanSums {
+    int64_t x[kPageThreads / 64], y[kPageThreads / 64];
+};
+
+__device__ __forceinline__ void scan_block(int64_t &x, int64_t &y, ScanSums &sums, int64_t &all_x, int64_t &all_y) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    int64_t ix = x, iy = y;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
-        const int64_t v = __shfl_up(incl, off);
-        if (lane >= off) incl += v;
+        const int64_t u = __shfl_up(ix, off), v = __shfl_up(iy, off);
+        if (lane >= off) {
+            ix += u;
+            iy += v;
+        }
     }
-    __syncthreads();  // the previous scan's sums have been read
-    if (lane == 63) sums[wave] = incl;
+    if (lane == 63) {
+        sums.x[wave] = ix;
+        sums.y[wave] = iy;
+    }
     __syncthreads();
-    int64_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < kPageThreads / 64; ++w) {
-        before += w < wave ? sums[w] : 0;
-        total += sums[w];
+    x = ix - x;
+    y = iy - y;
+    all_x = all_y = 0;
+    for (int w = 0; w < waves; ++w) {
+        if (w == wave) {
+            x += all_x;
+            y += all_y;
+        }
+        all_x += sums.x[w];
+        all_y += sums.y[w];
     }
-    return before + incl - x;
 }
 
-__device__ __forceinline__ int64_t pages_of(int64_t tokens, int page_size) {
-    return (tokens + page_size - 1) / page_size;
+// Sum over the workgroup's threads, in every thread.
+__device__ __forceinline__ int sum_block(int x, int *sums) {
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = x;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < (int)(blockDim.x >> 6); ++w) all += sums[w];
+    return all;
+}
+
+// tokens <= INT32_MAX, page_size >= 1
+__device__ __forceinline__ int pages_of(int tokens, int page_size) {
+    return (int)(((uint32_t)tokens + (uint32_t)page_size - 1u) / (uint32_t)page_size);
 }
 
 struct ExtendArgs {
@@ -67,52 +100,6 @@ struct ExtendArgs {
 
 __device__ __forceinline__ int clamp_count(int n, int pool) { return n < 0 ? 0 : (n > pool ? pool : n); }
 
-__global__ __launch_bounds__(kPageThreads) void extend_scan_kernel(ExtendArgs a) {
-    __shared__ int64_t sums[kPageThreads / 64];
-    const int tid = threadIdx.x;
-    const int per = (a.B + kPageThreads - 1) / kPageThreads;
-    const int b0 = tid * per < a.B ? tid * per : a.B;
-    const int b1 = b0 + per < a.B ? b0 + per : a.B;
-    const int64_t room = (int64_t)a.max_blocks * a.page_size;
-    auto want = [&](int b, int64_t &len, int64_t &fresh) -> int64_t {  // pages of b, -1: beyond its table row
-        len = a.lens[b] < 0 ? 0 : a.lens[b];
-        fresh = a.new_tokens[b] < 0 ? 0 : a.new_tokens[b];
-        if (fresh == 0) return 0;
-        const int64_t end = len + fresh;
-        return end > room || end > INT32_MAX ? -1 : pages_of(end, a.page_size) - pages_of(len, a.page_size);
-    };
-    int64_t need = 0, tokens = 0, len, fresh;
-    for (int b = b0; b < b1; ++b) {
-        const int64_t w = want(b, len, fresh);
-        need += w > 0 ? w : 0;
-        tokens += fresh;
-    }
-    int64_t all_need, all_tokens;
-    int64_t page = scan_block(need, sums, all_need), tok = scan_block(tokens, sums, all_tokens);
-    const int n = clamp_count(*a.n_free, a.pool);
-    int64_t mine = 0;
-    for (int b = b0; b < b1; ++b) {
-        const int64_t w = want(b, len, fresh);
-        const bool ok = w >= 0 && page + w <= n && tok + fresh <= a.max_tokens;
-        a.cu[b] = tok > INT32_MAX ? INT32_MAX : (int)tok;
-        a.st.first[b] = page > n ? n : (int)page;
-        a.st.len[b] = (int)len;
-        a.st.given[b] = ok ? (int)w : -1;
-        a.lens_out[b] = ok && fresh > 0 ? (int)(len + fresh) : a.lens[b];
-        mine += ok ? w : 0;
-        page += w > 0 ? w : 0;
-        tok += fresh;
-    }
-    int64_t given;
-    scan_block(mine, sums, given);
-    if (tid == 0) {
-        a.cu[a.B] = all_tokens > INT32_MAX ? INT32_MAX : (int)all_tokens;
-        a.st.head[0] = n;
-        a.st.head[1] = (int)given;
-        *a.n_free_out = n - (int)given;
-    }
-}
-
 // last b with v[b] <= x (v[0] <= x, v not decreasing)
 __device__ __forceinline__ int last_at_most(const int32_t *v, int B, int x) {
     int lo = 0, hi = B - 1;
@@ -123,27 +110,29 @@ __device__ __forceinline__ int last_at_most(const int32_t *v, int B, int x) {
     return lo;
 }
 
-__global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(ExtendArgs a) {
-    const int64_t id = (int64_t)blockIdx.x * kFillThreads + threadIdx.x;
-    const int64_t threads = (int64_t)gridDim.x * kFillThreads;
-    const int n = a.st.head[0], given = a.st.head[1], total = a.cu[a.B];
+// The flat pass, by `threads` threads of which this is `id`.  n: free pages before,
+// given: pages handed out; first, len, given_of and cu as the sums left them.
+__device__ __forceinline__ void extend_fill(const ExtendArgs &a, int64_t id, int64_t threads, int per, int n, int given,
+                                            const int32_t *first, const int32_t *len, const int32_t *given_of,
+                                            const int32_t *cu) {
+    const int total = cu[a.B];
     for (int64_t q = id; q < given; q += threads) {  // pages handed out
-        const int b = last_at_most(a.st.first, a.B, (int)q);
-        const int64_t col = pages_of(a.st.len[b], a.page_size) + (q - a.st.first[b]);
+        const int b = last_at_most(first, a.B, (int)q);
+        const int64_t col = pages_of(len[b], a.page_size) + (q - first[b]);
         a.table[(int64_t)b * a.max_blocks + col] = a.free_pages[n - 1 - q];
     }
-    for (int64_t i0 = id * kFillTokens; i0 < a.max_tokens; i0 += threads * kFillTokens) {
-        int b = i0 < total ? last_at_most(a.cu, a.B, (int)i0) : 0;
-        for (int64_t i = i0; i < i0 + kFillTokens && i < a.max_tokens; ++i) {
+    for (int64_t i0 = id * per; i0 < a.max_tokens; i0 += threads * per) {
+        int b = i0 < total ? last_at_most(cu, a.B, (int)i0) : 0;
+        for (int64_t i = i0; i < i0 + per && i < a.max_tokens; ++i) {
             int64_t slot = -1;
             int pos = 0;
             if (i < total) {
-                while (a.cu[b + 1] <= i) ++b;
-                if (a.st.given[b] >= 0) {
-                    pos = a.st.len[b] + (int)(i - a.cu[b]);
-                    const int64_t col = pos / a.page_size, held = pages_of(a.st.len[b], a.page_size);
+                while (cu[b + 1] <= i) ++b;
+                if (given_of[b] >= 0) {
+                    pos = len[b] + (int)(i - cu[b]);
+                    const int col = (int)((uint32_t)pos / (uint32_t)a.page_size), held = pages_of(len[b], a.page_size);
                     const int page = col < held ? a.table[(int64_t)b * a.max_blocks + col]
-                                                : a.free_pages[n - 1 - (a.st.first[b] + (col - held))];
+                                                : a.free_pages[n - 1 - (first[b] + (col - held))];
                     if (page >= 0) slot = (int64_t)page * a.page_size + (pos - col * a.page_size);
                 }
             }
@@ -151,6 +140,78 @@ __global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(ExtendArgs a)
             a.positions[i] = pos;
         }
     }
+}
+
+// ONE: the flat pass too, from sums in LDS (B <= kOneLaunchB).  PER: most sequences a
+// thread; they are held in registers, so that their loads overlap.
+template <bool ONE, int PER>
+__global__ __launch_bounds__(kPageThreads) void extend_scan_kernel(ExtendArgs a) {
+    __shared__ ScanSums sums;
+    __shared__ int given_sums[kPageThreads / 64];
+    __shared__ int32_t local[ONE ? 4 * kOneLaunchB + 1 : 1];
+    int32_t *const first = ONE ? local : a.st.first, *const lens = ONE ? local + kOneLaunchB : a.st.len;
+    int32_t *const given_of = ONE ? local + 2 * kOneLaunchB : a.st.given, *const cu = ONE ? local + 3 * kOneLaunchB : a.cu;
+    const int tid = threadIdx.x;
+    const int per = (a.B + (int)blockDim.x - 1) / (int)blockDim.x;
+    const int b0 = tid * per < a.B ? tid * per : a.B;
+    const int b1 = b0 + per < a.B ? b0 + per : a.B;
+    const int64_t room = (int64_t)a.max_blocks * a.page_size;
+    auto want = [&](int b, int &len, int &fresh) -> int {  // pages of b, -1: beyond its table row
+        len = a.lens[b] < 0 ? 0 : a.lens[b];
+        fresh = a.new_tokens[b] < 0 ? 0 : a.new_tokens[b];
+        if (fresh == 0) return 0;
+        const int64_t end = (int64_t)len + fresh;
+        return end > room || end > INT32_MAX ? -1 : pages_of((int)end, a.page_size) - pages_of(len, a.page_size);
+    };
+    const int n = clamp_count(*a.n_free, a.pool);
+    int64_t page = 0, tok = 0, all_need, all_tokens;
+    int len[PER], fresh[PER], want_of[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (b0 + j >= b1) continue;
+        want_of[j] = want(b0 + j, len[j], fresh[j]);
+        page += want_of[j] > 0 ? want_of[j] : 0;
+        tok += fresh[j];
+    }
+    scan_block(page, tok, sums, all_need, all_tokens);
+    int mine = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int b = b0 + j, w = want_of[j];
+        if (b >= b1) continue;
+        const bool ok = w >= 0 && page + w <= n && tok + fresh[j] <= a.max_tokens;
+        const int at = tok > INT32_MAX ? INT32_MAX : (int)tok;
+        cu[b] = at;
+        if (ONE) a.cu[b] = at;
+        first[b] = page > n ? n : (int)page;
+        lens[b] = len[j];
+        given_of[b] = ok ? w : -1;
+        if (ok && fresh[j] > 0) a.lens_out[b] = len[j] + fresh[j];
+        else if (a.lens_out != a.lens) a.lens_out[b] = a.lens[b];
+        mine += ok ? w : 0;
+        page += w > 0 ? w : 0;
+        tok += fresh[j];
+    }
+    const int given = sum_block(mine, given_sums);  // and every thread's sums are written
+    if (tid == 0) {
+        const int at = all_tokens > INT32_MAX ? INT32_MAX : (int)all_tokens;
+        a.cu[a.B] = at;
+        if (ONE) cu[a.B] = at;
+        if (!ONE) {
+            a.st.head[0] = n;
+            a.st.head[1] = given;
+        }
+        *a.n_free_out = n - given;
+    }
+    if (ONE) {
+        __syncthreads();
+        extend_fill(a, tid, blockDim.x, 1, n, given, first, lens, given_of, cu);
+    }
+}
+
+__global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(ExtendArgs a) {
+    extend_fill(a, (int64_t)blockIdx.x * kFillThreads + threadIdx.x, (int64_t)gridDim.x * kFillThreads, kFillTokens,
+                a.st.head[0], a.st.head[1], a.st.first, a.st.len, a.st.given, a.cu);
 }
 
 struct ReleaseArgs {
@@ -162,33 +223,40 @@ struct ReleaseArgs {
     PageState st;
 };
 
+template <int PER>
 __global__ __launch_bounds__(kPageThreads) void release_scan_kernel(ReleaseArgs a) {
-    __shared__ int64_t sums[kPageThreads / 64];
+    __shared__ ScanSums sums;
     const int tid = threadIdx.x;
-    const int per = (a.B + kPageThreads - 1) / kPageThreads;
+    const int per = (a.B + (int)blockDim.x - 1) / (int)blockDim.x;
     const int b0 = tid * per < a.B ? tid * per : a.B;
     const int b1 = b0 + per < a.B ? b0 + per : a.B;
-    auto cut = [&](int b, int &kept, int64_t &c0) -> int64_t {  // pages of b that go back, from column c0
+    auto cut = [&](int b, int &kept, int &c0) -> int {  // pages of b that go back, from column c0
         const int len = a.lens[b], keep = a.keep[b] < 0 ? 0 : a.keep[b];
         kept = keep < len ? keep : len;
         c0 = pages_of(kept > 0 ? kept : 0, a.page_size);
-        int64_t c1 = pages_of(len > 0 ? len : 0, a.page_size);
+        int c1 = pages_of(len > 0 ? len : 0, a.page_size);
         if (c1 > a.max_blocks) c1 = a.max_blocks;
         return c1 > c0 ? c1 - c0 : 0;
     };
-    int64_t mine = 0, c0, all;
-    int kept;
-    for (int b = b0; b < b1; ++b) mine += cut(b, kept, c0);
-    int64_t at = scan_block(mine, sums, all);
     const int n = clamp_count(*a.n_free, a.pool);
+    int64_t at = 0, unused = 0, all, all_unused;
+    int kept[PER], c0[PER], c[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        if (b0 + j >= b1) continue;
+        c[j] = cut(b0 + j, kept[j], c0[j]);
+        at += c[j];
+    }
+    scan_block(at, unused, sums, all, all_unused);
     const int64_t room = a.pool - n;
-    for (int b = b0; b < b1; ++b) {
-        const int64_t c = cut(b, kept, c0);
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int b = b0 + j;
+        if (b >= b1) continue;
         a.st.first[b] = at > room ? (int)room : (int)at;
-        a.st.len[b] = (int)(c0 > a.max_blocks ? a.max_blocks : c0);
-        a.st.given[b] = (int)c;
-        a.lens_out[b] = kept;
-        at += c;
+        a.st.len[b] = c0[j] > a.max_blocks ? a.max_blocks : c0[j];
+        a.lens_out[b] = kept[j];
+        at += c[j];
     }
     __syncthreads();
     if (tid == 0) {
@@ -209,6 +277,9 @@ __global__ __launch_bounds__(kFillThreads) void release_fill_kernel(ReleaseArgs 
 
 size_t page_workspace_bytes(int B) { return 4 * (64 + 3 * (((size_t)B + 63) & ~(size_t)63)); }
 
+// whole waves for B sequences
+static unsigned scan_threads(int B) { return (unsigned)(B < 1 ? 64 : (B + 63) / 64 * 64); }
+
 static unsigned fill_grid(int64_t items) {
     const int64_t g = (items + kFillThreads - 1) / kFillThreads;
     return (unsigned)(g < 1 ? 1 : (g > 4096 ? 4096 : g));
@@ -218,7 +289,13 @@ hipError_t launch_page_extend(const PageExtend &x, hipStream_t st) {
     ExtendArgs a{x.table, x.lens, x.new_tokens, x.free_pages, x.n_free, x.slots, x.positions, x.cu,
                  x.lens_out, x.n_free_out, x.B, x.page_size, x.max_blocks, x.pool, x.max_tokens,
                  page_state(x.ws, x.B)};
-    hipLaunchKernelGGL(extend_scan_kernel, dim3(1), dim3(kPageThreads), 0, st, a);
+    if (x.B > kPageThreads * kPagePer) return hipErrorInvalidValue;
+    if (x.B <= kOneLaunchB && x.max_tokens <= kOneLaunchTokens) {
+        hipLaunchKernelGGL((extend_scan_kernel<true, 1>), dim3(1), dim3(kPageThreads), 0, st, a);
+        return hipGetLastError();
+    }
+    if (x.B <= kPageThreads) hipLaunchKernelGGL((extend_scan_kernel<false, 1>), dim3(1), dim3(scan_threads(x.B)), 0, st, a);
+    else hipLaunchKernelGGL((extend_scan_kernel<false, kPagePer>), dim3(1), dim3(kPageThreads), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(extend_fill_kernel, dim3(fill_grid(x.max_tokens / kFillTokens + x.B)), dim3(kFillThreads), 0, st, a);
@@ -228,7 +305,9 @@ hipError_t launch_page_extend(const PageExtend &x, hipStream_t st) {
 hipError_t launch_page_release(const PageRelease &x, hipStream_t st) {
     ReleaseArgs a{x.table, x.lens, x.keep, x.free_pages, x.n_free, x.lens_out, x.n_free_out, x.B,
                   x.page_size, x.max_blocks, x.pool, page_state(x.ws, x.B)};
-    hipLaunchKernelGGL(release_scan_kernel, dim3(1), dim3(kPageThreads), 0, st, a);
+    if (x.B > kPageThreads * kPagePer) return hipErrorInvalidValue;
+    if (x.B <= kPageThreads) hipLaunchKernelGGL(release_scan_kernel<1>, dim3(1), dim3(scan_threads(x.B)), 0, st, a);
+    else hipLaunchKernelGGL(release_scan_kernel<kPagePer>, dim3(1), dim3(kPageThreads), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL(release_fill_kernel, dim3(fill_grid((int64_t)x.B * 4)), dim3(kFillThreads), 0, st, a);
