@@ -189,27 +189,18 @@ def kv_view(k: torch.Tensor, v: torch.Tensor, block_table: Optional[torch.Tensor
     """Describe 4-d storage [blk, h, tok, d] (d contiguous) as a spire_kv.
     Paged when `block_table` is given (blk = physical page), else contiguous
     (blk = sequence, capacity = size of dim 2 unless given)."""
-    assert k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype
-    assert k.stride(3) == 1, "head dim must be contiguous"
-    kv = KV()
-    kv.k, kv.v = k.data_ptr(), v.data_ptr()
-    kv.s_blk, kv.s_head, kv.s_tok = k.stride(0), k.stride(1), k.stride(2)
-    kv.dtype = _DT[k.dtype]
-    kv.k_scale, kv.v_scale = _ptr(k_scale), _ptr(v_scale)
+    shape, stride = k.shape, k.stride()
+    assert shape == v.shape and stride == v.stride() and k.dtype == v.dtype
+    assert stride[3] == 1, "head dim must be contiguous"
+    table, rows, columns = None, 0, 0
     if block_table is not None:
         assert block_table.dtype == torch.int32 and block_table.is_contiguous()
-        kv.block_table = block_table.data_ptr()
-        kv.page_size = page_size or k.shape[2]
-        kv.max_blocks = block_table.shape[1]
-        kv.num_blocks = k.shape[0]
-        kv.capacity = 0
-    else:
-        kv.block_table = None
-        kv.page_size = 0
-        kv.num_blocks = k.shape[0]
-        kv.capacity = k.shape[2] if capacity is None else capacity
-    kv.reserved = 0
-    return kv
+        table, rows, columns, capacity = block_table.data_ptr(), page_size or shape[2], block_table.shape[1], 0
+    elif capacity is None:
+        capacity = shape[2]
+    # the fields in one call: one by one they are a third of a small call's time
+    return KV(k.data_ptr(), v.data_ptr(), table, _ptr(k_scale), _ptr(v_scale), stride[0], stride[1], stride[2],
+              _DT[k.dtype], rows, columns, shape[0], capacity, 0)
 
 
 def verify_workspace_size(B, Hq, Hkv, D, k) -> int:
@@ -488,15 +479,13 @@ def rope_view(positions: torch.Tensor, inv_freq: torch.Tensor, axis: Optional[to
     axis [rot_dim / 2] int32 (the position axis of each pair) or None for axis 0."""
     _ints(positions)
     assert inv_freq.dtype == torch.float32 and inv_freq.is_contiguous()
-    r = Rope()
-    r.positions, r.inv_freq = positions.data_ptr(), inv_freq.data_ptr()
+    pairs, shape = inv_freq.numel(), positions.shape
     if axis is not None:
         _ints(axis)
-        assert axis.numel() == inv_freq.numel()
-        r.axis = axis.data_ptr()
-    r.axes = positions.shape[0] if positions.dim() == 2 else 1
-    r.rot_dim, r.interleaved, r.reserved = 2 * inv_freq.numel(), int(interleaved), 0
-    r.tokens = positions.shape[-1]  # of this wrapper alone: the calls check it against N
+        assert axis.numel() == pairs
+    r = Rope(positions.data_ptr(), inv_freq.data_ptr(), _ptr(axis), shape[0] if len(shape) == 2 else 1, 2 * pairs,
+             interleaved, 0)
+    r.tokens = shape[-1]  # of this wrapper alone: the calls check it against N
     r.keep = (positions, inv_freq, axis)
     return r
 
@@ -516,19 +505,19 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv: KV, slots:
     stride), slots [N] int64, weights [D] fp32; returns q_out [N, Hq, D]."""
     N, Hq, D = q.shape
     Hkv = k.shape[1]
-    assert k.shape == (N, Hkv, D) and v.shape == k.shape and q.dtype == k.dtype == v.dtype
-    for t in (q, k, v):
-        assert t.stride(2) == 1 and t.stride(1) == D, "heads must be contiguous"
+    dtype = q.dtype
+    assert k.shape == (N, Hkv, D) and v.shape == k.shape and k.dtype == dtype and v.dtype == dtype
+    (qs, qh, qd), (ks, kh, kd), (vs, vh, vd) = q.stride(), k.stride(), v.stride()
+    assert qh == kh == vh == D and qd == kd == vd == 1, "heads must be contiguous"
     assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == N
     for w in (q_weight, k_weight):
         assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == D)
     if q_out is None:
-        q_out = torch.empty((N, Hq, D), dtype=out_dtype or q.dtype, device=q.device)
-    assert q_out.shape == q.shape and q_out.is_contiguous()
-    _check(load().spire_qkv_append(q.data_ptr(), q.stride(0), k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0),
-                                   _DT[q.dtype], _ptr(q_weight), _ptr(k_weight), float(eps), _rope(rope, N),
-                                   C.byref(kv), slots.data_ptr(), N, Hq, Hkv, D, q_out.data_ptr(),
-                                   _DT[q_out.dtype], _stream()))
+        q_out = torch.empty((N, Hq, D), dtype=out_dtype or dtype, device=q.device)
+    assert q_out.shape == (N, Hq, D) and q_out.is_contiguous()
+    _check(load().spire_qkv_append(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, _DT[dtype], _ptr(q_weight),
+                                   _ptr(k_weight), eps, _rope(rope, N), C.byref(kv), slots.data_ptr(), N, Hq, Hkv, D,
+                                   q_out.data_ptr(), _DT[q_out.dtype], _stream()))
     return q_out
 
 
@@ -537,16 +526,16 @@ def latent_view(cache: torch.Tensor, Dc: int, block_table: Optional[torch.Tensor
     """Describe 3-d storage [blk, tok, Dc + Dr] (last dimension contiguous) as a spire_latent.  Paged when
     `block_table` is given (blk = physical page, tok = row of the page), else contiguous (blk = sequence,
     capacity = size of dim 1 unless given)."""
-    assert cache.dim() == 3 and cache.stride(2) == 1 and 0 < Dc < cache.shape[2]
-    c = Latent()
-    c.c, c.dtype, c.Dc, c.Dr = cache.data_ptr(), _DT[cache.dtype], Dc, cache.shape[2] - Dc
-    c.s_blk, c.s_tok, c.num_blocks = cache.stride(0), cache.stride(1), cache.shape[0]
-    c.scale = _ptr(scale)
+    (blocks, tokens, Dk), (s_blk, s_tok, s_d) = cache.shape, cache.stride()
+    assert s_d == 1 and 0 < Dc < Dk
+    table, rows, columns = None, 0, 0
     if block_table is not None:
         _ints(block_table)
-        c.block_table, c.page_size, c.max_blocks = block_table.data_ptr(), cache.shape[1], block_table.shape[1]
-    else:
-        c.capacity = cache.shape[1] if capacity is None else capacity
+        table, rows, columns, capacity = block_table.data_ptr(), tokens, block_table.shape[1], 0
+    elif capacity is None:
+        capacity = tokens
+    c = Latent(cache.data_ptr(), table, _ptr(scale), s_blk, s_tok, _DT[cache.dtype], Dc, Dk - Dc, rows, columns,
+               blocks, capacity, 0)
     c.keep = (cache, block_table, scale)
     return c
 
@@ -556,20 +545,20 @@ def latent_append(latent: Latent, c: torch.Tensor, k_rope: torch.Tensor, slots: 
                   q_rope: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None):
     """spire_latent_append.  c [N, Dc], k_rope [N, Dr], q_rope [N, Hq, Dr] (fp32 or bf16, any token and head
     strides), slots [N] int64, weight [Dc] fp32; q [N, Hq, Dc + Dr] gets the rotated parts in its last Dr."""
-    N, Dc = c.shape
-    assert Dc == latent.Dc and k_rope.shape == (N, latent.Dr) and k_rope.dtype == c.dtype
-    assert c.stride(1) == 1 and k_rope.stride(1) == 1
+    (N, Dc), Dr, dtype = c.shape, latent.Dr, c.dtype
+    (cs, cd), (ks, kd) = c.stride(), k_rope.stride()
+    assert Dc == latent.Dc and k_rope.shape == (N, Dr) and k_rope.dtype == dtype and cd == kd == 1
     assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == N
     assert weight is None or (weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == Dc)
-    Hq, qs, qh, qp, op, od = 0, 0, 0, None, None, c.dtype
+    Hq, qs, qh, qp, op, od = 0, 0, 0, None, None, dtype
     if q_rope is not None:
-        Hq = q_rope.shape[1]
-        assert q_rope.shape == (N, Hq, latent.Dr) and q_rope.dtype == c.dtype and q_rope.stride(2) == 1
-        assert q.shape == (N, Hq, Dc + latent.Dr) and q.is_contiguous()
-        qs, qh, qp, op, od = q_rope.stride(0), q_rope.stride(1), q_rope.data_ptr(), q.data_ptr(), q.dtype
-    _check(load().spire_latent_append(c.data_ptr(), c.stride(0), k_rope.data_ptr(), k_rope.stride(0), qp, qs, qh,
-                                      _DT[c.dtype], _ptr(weight), float(eps), _rope(rope, N), C.byref(latent),
-                                      slots.data_ptr(), N, Hq, op, _DT[od], _stream()))
+        Hq, (qs, qh, qd) = q_rope.shape[1], q_rope.stride()
+        assert q_rope.shape == (N, Hq, Dr) and q_rope.dtype == dtype and qd == 1
+        assert q.shape == (N, Hq, Dc + Dr) and q.is_contiguous()
+        qp, op, od = q_rope.data_ptr(), q.data_ptr(), q.dtype
+    _check(load().spire_latent_append(c.data_ptr(), cs, k_rope.data_ptr(), ks, qp, qs, qh, _DT[dtype], _ptr(weight),
+                                      eps, _rope(rope, N), C.byref(latent), slots.data_ptr(), N, Hq, op, _DT[od],
+                                      _stream()))
 
 
 def latent_workspace_size(B, Hq, k, Dc, Dr) -> int:
