@@ -44,7 +44,7 @@ __global__ __launch_bounds__(256) void latent_f32_kernel(Latent a) {
 
     while (pos < end) {
         const int b = seg;
-        const int n = effective_keys(p, b), tiles = latent_tiles(n), span = tiles + pl.seg_cost;
+        const int n = effective_keys(p, b), tiles = latent_tiles<kLatF32Tile>(n), span = tiles + pl.seg_cost;
         const int64_t left = end - pos;
         const int te = left < (int64_t)(span - tile) ? tile + (int)left : span;
         if (tile < tiles) {

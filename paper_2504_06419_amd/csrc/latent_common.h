@@ -54,6 +54,7 @@ __device__ __forceinline__ bool latent_start(const Latent &a, int g, int u, int3
 }
 
 // Positions of sequence b: its tiles and the phantoms of its segment.
-__device__ __forceinline__ int latent_tiles(int n) { return n > 0 ? (n + kLatentTile - 1) / kLatentTile : 1; }
+template <int TILE>
+__device__ __forceinline__ int latent_tiles(int n) { return n > 0 ? (n + TILE - 1) / TILE : 1; }
 
 }  // namespace spire

@@ -104,13 +104,11 @@ __device__ __forceinline__ cLatent *arguments() {
     return (cLatent *)x;
 }
 
-constexpr int kLatKT = kLatentTile / 16;  // 16-key blocks a tile
-
 // Stage of one tile: [TILE][DC] rows, then [TILE][64] rotated parts.  16-byte chunk q of
 // row r lies at q ^ fm(r) (main part, low 4 bits) and q ^ fr(r): operand reads (16
 // rows, one chunk) and transposing reads (4 rows, 2 chunks) hit distinct banks.
-template <int DC, bool FP8, int CW> struct LatStage {  // CW: waves that copy
-    static constexpr int KT = kLatKT, TILE = 16 * KT;
+template <int DC, bool FP8, int CW, int TILE_> struct LatStage {  // CW: waves that copy
+    static constexpr int TILE = TILE_, KT = TILE / 16;  // 16-key blocks
     static constexpr int ES = FP8 ? 1 : 2;
     static constexpr int RB = DC * ES, RR = kLatentDr * ES;  // bytes of a row's parts
     static constexpr int MAIN = TILE * RB;
@@ -129,10 +127,10 @@ template <int PR> __device__ __forceinline__ int fp(int r) { return PR == 64 ? (
 template <int DC, bool FP8, int NB>
 __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
     // Waves without rows to score copy the tiles; with 7 and 8 blocks every wave does its share.
-    constexpr int CW = NB <= 4 ? 4 : (NB <= 6 ? 2 : 8), SCAN = kLatentTile / 8;  // copying waves; rows a wave looks through
-    using G = LatStage<DC, FP8, CW>;
+    constexpr int CW = NB <= 4 ? 4 : (NB <= 6 ? 2 : 8), TILE = latent_tile(true, DC * (FP8 ? 1 : 2), NB), SCAN = TILE / 8;  // copying waves; rows a wave looks through
+    using G = LatStage<DC, FP8, CW, TILE>;
     constexpr bool NT = NB <= 4;  // up to 4 blocks are one unit: its rows are read once, and streamed
-    constexpr int DK = DC + kLatentDr, TILE = G::TILE, KT = G::KT;
+    constexpr int DK = DC + kLatentDr, KT = G::KT;
     constexpr int STEPS = DK / 32;      // QK steps of 32 dimensions
     constexpr int XB = DC / 128;        // 16-dimension output blocks of a wave
     constexpr int PB = NB * 16 * G::PR;
@@ -191,7 +189,7 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
 
     while (pos < end) {
         const int b = seg;
-        const int n = effective_keys(p, b), tiles = latent_tiles(n), span = tiles + pl.seg_cost;
+        const int n = effective_keys(p, b), tiles = latent_tiles<TILE>(n), span = tiles + pl.seg_cost;
         const int64_t left = end - pos;
         const int te = left < (int64_t)(span - tile) ? tile + (int)left : span;
         if (tile >= tiles) {  // phantom positions only

@@ -1119,11 +1119,12 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
     a.uniform = latent->page_size % 16 == 0;
     a.quads = (uintptr_t)latent->c % (4 * es) == 0 && latent->s_blk % 4 == 0 && latent->s_tok % 4 == 0;
     Plan &pl = a.pl;
-    pl.tile = kLatentTile;
+    pl.tile = latent_tile(matrix, p.D * es, sh.nb);
     pl.units = 1;
     pl.rows = sh.units * sh.nb * 16;
     pl.workers = sh.groups;
-    pl.seg_cost = matrix ? 6 : 0;
+    // A segment's start and end against its tiles, in keys (64 sequences, 80 rows: 100 us with 192, 95 with 384).
+    pl.seg_cost = matrix ? 384 / pl.tile : 0;
     const Layout L = latent_layout(B, p.D, sh);
     if (workspace_bytes < L.total)
         return fail(SPIRE_ERR_WORKSPACE, "workspace has %zu bytes, needs %zu", workspace_bytes, L.total);

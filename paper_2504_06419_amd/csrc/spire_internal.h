@@ -315,7 +315,12 @@ hipError_t launch_qkv_append(const QkvAppend &x, hipStream_t st);
 hipError_t launch_latent_append(const LatentAppend &x, hipStream_t st);
 
 // ---- latent attention (latent_common.h, latent_attn.hip) ----------------------------
-constexpr int kLatentTile = 32;  // keys a tile, both kernels
+// Keys a tile.  A tile's barriers and exchanges take a time of their own, which shows where
+// a tile is little work otherwise: rows of up to 512 bytes and up to 64 query rows take
+// tiles of 64 keys (64 sequences of 16384 rows, 16 heads; 512 fp8: 167 us with 32 keys, 134
+// with 64; 64 query rows 212 and 184; 256 bf16, 64 rows: 152 and 130).
+constexpr int kLatentTile = 32;
+constexpr int latent_tile(bool matrix, int latent_bytes, int nb) { return matrix && latent_bytes <= 512 && nb <= 4 ? 64 : kLatentTile; }
 constexpr int kLatentDr = 64;  // rotated elements of a row
 struct Latent {
     Problem p;        // Hkv = 1, D = Dc, kv = the latent view (k, k_scale)
