@@ -96,7 +96,7 @@ typedef struct spire_kv {
     int32_t dtype;               /* spire_dtype */
     int32_t page_size;           /* 0 = contiguous; paged: tokens per page */
     int32_t max_blocks;          /* paged: columns of block_table */
-    int32_t num_blocks;          /* paged: physical pages addressable in k / v */
+    int32_t num_blocks;          /* paged: physical pages addressable in k / v; contiguous: sequences (read by spire_qkv_append alone) */
     int32_t capacity;            /* contiguous: token rows per sequence */
     int32_t reserved;            /* must be 0 */
 } spire_kv;
@@ -446,7 +446,7 @@ typedef struct spire_rope {
  *   kv    destination view; paged, or contiguous with num_blocks = its sequences.
  *     Written at slots[t] (the block table is not read); rounded as for
  *     spire_kv_append.  A slot outside [0, num_blocks * rows per block) is
- *     skipped; two tokens with one slot leave either's row.
+ *     skipped; two tokens with one slot leave, element by element, either's row.
  *   sizes  0 <= N < 2^31, 1 <= Hq, 1 <= Hkv, Hq + 2 Hkv <= 4096, 1 <= D <= 1024.
  * Arithmetic in fp32, one rounding per stored element.  Outputs must not
  * overlap inputs.  No workspace.

@@ -136,6 +136,11 @@ def test_split_sequences(Hq, k, lens, kv):
     check(inp)
 
 
+@pytest.mark.parametrize("kernel,Dc,kv", [(0, 512, "fp8"), (0, 256, "bf16"), (1, 256, "bf16")])
+def test_most_sequences(kernel, Dc, kv):
+    check(Inp([i % 40 for i in range(8192)], 4, 0, Dc=Dc, kv=kv, seed=8), "bf16", kernel)
+
+
 @pytest.mark.parametrize("kernel", [0, 1])
 @pytest.mark.parametrize("kv", ["bf16", "fp8"])
 def test_large_scores(kernel, kv):

@@ -66,6 +66,14 @@ def test_extend(B, ps, hi, new_hi, in_place):
     assert c.gpu(in_place) == tuple(c.want())
 
 
+@pytest.mark.parametrize("B,ps,hi,new_hi", [(1000, 16, 90, 2), (1024, 4, 300, 1), (200, 1, 40, 18), (200, 8, 40, 30), (3, 16, 50, 600),
+                                            (8192, 16, 90, 0)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_extend_in_one_launch_and_two(B, ps, hi, new_hi, in_place):
+    c = Case(7 * B + ps, B, ps, hi, new_hi)
+    assert c.gpu(in_place) == tuple(c.want())
+
+
 @pytest.mark.parametrize("slack,tokens,maxb", [(6, None, None), (40, None, None), (0, 20, None), (0, 0, None), (0, None, 6),
                                                (10**6, None, None), (-50, None, None)])
 def test_extend_refuses(slack, tokens, maxb):

@@ -208,6 +208,33 @@ def test_latent_layouts(kw):
     run_latent(**dict(dict(N=13, Hq=16, Dc=512, Dr=64, seed=5), **kw))
 
 
+@pytest.mark.parametrize("N,Hq,Hkv,D,rot", [(1500, 32, 8, 128, 128), (1501, 33, 3, 128, 64), (4100, 5, 3, 128, 128),
+                                            (900, 20, 4, 256, 256), (700, 12, 2, 512, 64), (2900, 32, 8, 64, 64)])
+@pytest.mark.parametrize("kw", [dict(), dict(kv="fp8", axes=3, inter=True), dict(new="f32", kv="f32", norm=False)])
+def test_several_rounds_a_wave(N, Hq, Hkv, D, rot, kw):
+    run_qkv(N, Hq, Hkv, D, rot, seed=N, **kw)
+
+
+@pytest.mark.parametrize("N,Hq,Dc,Dr", [(2000, 128, 512, 64), (4100, 16, 256, 64), (1111, 100, 512, 32), (4100, 31, 128, 128)])
+@pytest.mark.parametrize("kw", [dict(), dict(kv="fp8", inter=False), dict(new="f32", kv="bf16")])
+def test_latent_several_rounds_a_wave(N, Hq, Dc, Dr, kw):
+    run_latent(N, Hq, Dc, Dr, seed=N, **kw)
+
+
+def test_one_slot_twice():
+    """Two tokens of one slot: every stored element is the one's or the other's."""
+    g = gen(5)
+    N, D = 64, 128
+    x = randn(g, N, 3, D, dt=torch.bfloat16)
+    c = torch.zeros(2, 1, 16, D, device=DEV, dtype=torch.bfloat16)
+    d, table = c.clone(), torch.zeros(1, 1, dtype=torch.int32, device=DEV)
+    slots = torch.arange(N, device=DEV) // 2
+    spire.qkv_append(x[:, :1], x[:, 1:2], x[:, 2:], spire.kv_view(c, d, table, 16), slots)
+    for cache, h in ((c, 1), (d, 2)):
+        got = cache[:, 0].reshape(32, D)
+        assert torch.all((got == x[0::2, h]) | (got == x[1::2, h]))
+
+
 def test_in_a_graph_and_on_another_stream():
     g = gen(8)
     N, Hq, Hkv, D = 40, 8, 2, 128
