@@ -384,12 +384,16 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                if ((wave ^ 1) < NB) {
+                if (NB % 2 == 0 || (wave ^ 1) < NB) {
                     const uint32_t at = x0 + (half ? -16 * G::PR : 16 * G::PR) + 16 * here(lane);  // the partner's block
 #pragma unroll
                     for (int y = 0; y < KT; ++y)
                         *reinterpret_cast<__attribute__((address_space(3))) f32x4 *>(
                             (lds_u8 *)(uintptr_t)(at + (y < KT / 2 ? buf * PB + 1024 * y : 2 * PB + 1024 * (y - KT / 2)))) = s[QB - 1][y];
+                } else if (NB > 1) {
+                    // The partner's scores are not used: nothing reads them, and the compiler does not
+                    // count the wait states (8) before their registers are written again on this way.
+                    asm volatile("s_nop 7" ::: "memory");
                 }
             };
 
