@@ -240,16 +240,15 @@ __device__ __forceinline__ void write_row(const Latent &a, int64_t qrow, int d, 
     if (d == 0 && p.lse != nullptr) p.lse[qrow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
 }
 
-// Few partials a sequence: DC / 4 threads a row walk them, kRows rows a workgroup.
-constexpr int kCombineRows = 8;
+// Few partials a sequence: DC / 4 threads a row walk them, `rows` rows a workgroup.
 template <int DC>
-__global__ __launch_bounds__(256) void latent_combine_kernel(Latent a, int per_group) {
+__global__ __launch_bounds__(256) void latent_combine_kernel(Latent a, int per_group, int rows) {
     constexpr int TPR = DC / 4, AT = 256 / TPR;  // threads a row, rows at a time
     const Plan &pl = a.pl;
     const Split s = split_of(a, blockIdx.x, per_group != 0);
     if (s.m == 0) return;
     const int d = 4 * (threadIdx.x % TPR);
-    for (int row = blockIdx.y * kCombineRows + threadIdx.x / TPR; row < (int)(blockIdx.y + 1) * kCombineRows; row += AT) {
+    for (int row = blockIdx.y * rows + threadIdx.x / TPR; row < (int)(blockIdx.y + 1) * rows; row += AT) {
         const int64_t qrow = query_row(a, s.b, row);
         if (qrow < 0) continue;
         // M: the largest log-sum-exp so far (-inf: none); sums are kept relative to it
@@ -377,10 +376,15 @@ hipError_t launch_latent_combine(const Latent &a, hipStream_t st) {
         else hipLaunchKernelGGL(latent_combine_wide_kernel<256>, grid, block, 0, st, a);
         return hipGetLastError();
     }
-    const int per_group = a.p.B > a.pl.workers;
-    const dim3 grid((unsigned)(per_group ? a.pl.workers : a.p.B), (unsigned)((a.pl.rows + kCombineRows - 1) / kCombineRows)), block(256);
-    if (big) hipLaunchKernelGGL(latent_combine_kernel<512>, grid, block, 0, st, a, per_group);
-    else hipLaunchKernelGGL(latent_combine_kernel<256>, grid, block, 0, st, a, per_group);
+    // Rows a workgroup: as few as fill the device (64 sequences of 16 rows: 8 rows 17.5 us, 2
+    // rows 9.0; of 80 rows: 22.2 and 17.7), 8 where there are many (128 sequences of 128
+    // rows: 29.6 us, 36.4 with 2), since each finds its sequence's partials first.
+    const int per_group = a.p.B > a.pl.workers, seqs = per_group ? a.pl.workers : a.p.B;
+    const int64_t total = (int64_t)seqs * a.pl.rows;
+    const int rows = total >= 16384 ? 8 : (total >= 8192 || !big ? 4 : 2);
+    const dim3 grid((unsigned)seqs, (unsigned)((a.pl.rows + rows - 1) / rows)), block(256);
+    if (big) hipLaunchKernelGGL(latent_combine_kernel<512>, grid, block, 0, st, a, per_group, rows);
+    else hipLaunchKernelGGL(latent_combine_kernel<256>, grid, block, 0, st, a, per_group, rows);
     return hipGetLastError();
 }
 
