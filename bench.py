@@ -517,6 +517,7 @@ KERNEL_SOURCES = ["paper_2504_06419_amd/csrc/attn_mfma.hip",
                   "paper_2504_06419_amd/csrc/block_verify.hip",
                   "paper_2504_06419_amd/csrc/sampling.h",
                   "paper_2504_06419_amd/csrc/kv_update.hip",
+                  "paper_2504_06419_amd/csrc/convert.h",
                   "paper_2504_06419_amd/csrc/feedback_memory.hip",
                   "paper_2504_06419_amd/csrc/mfma_common.h",
                   "paper_2504_06419_amd/csrc/spire_internal.h",
