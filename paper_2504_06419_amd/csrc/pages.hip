@@ -18,11 +18,11 @@ namespace spire {
 constexpr int kPageThreads = 1024;
 constexpr int kPagePer = 8;        // sequences a thread: B <= 8192
 constexpr int kOneLaunchB = 1024;  // sequences whose sums stand in LDS
-// Tokens up to which the flat pass is the scanning workgroup's own (256 sequences, 2048
-// tokens: 7.7 us, two launches 10.4; 4096 tokens: 9.9 and 9.4).
+// Tokens up to which the flat pass is the scanning workgroup's own.  256 sequences in one
+// launch and in two, on the device: 1024 tokens 6.6 and 6.5 us, 2048 7.5 and 6.6, 4096 9.5
+// and 6.7 (1024 sequences, 1024 tokens: 7.3 and 9.5); a launch costs the host 2.5 us.
 constexpr int kOneLaunchTokens = 2048;
 constexpr int kFillThreads = 256;
-constexpr int kFillTokens = 4;  // consecutive tokens per thread
 
 // What the prefix sums leave for the flat pass (workspace, B entries each).
 struct PageState {
@@ -112,7 +112,7 @@ __device__ __forceinline__ int last_at_most(const int32_t *v, int B, int x) {
 
 // The flat pass, by `threads` threads of which this is `id`.  n: free pages before,
 // given: pages handed out; first, len, given_of and cu as the sums left them.
-__device__ __forceinline__ void extend_fill(const ExtendArgs &a, int64_t id, int64_t threads, int per, int n, int given,
+__device__ __forceinline__ void extend_fill(const ExtendArgs &a, int64_t id, int64_t threads, int n, int given,
                                             const int32_t *first, const int32_t *len, const int32_t *given_of,
                                             const int32_t *cu) {
     const int total = cu[a.B];
@@ -121,24 +121,19 @@ __device__ __forceinline__ void extend_fill(const ExtendArgs &a, int64_t id, int
         const int64_t col = pages_of(len[b], a.page_size) + (q - first[b]);
         a.table[(int64_t)b * a.max_blocks + col] = a.free_pages[n - 1 - q];
     }
-    for (int64_t i0 = id * per; i0 < a.max_tokens; i0 += threads * per) {
-        int b = i0 < total ? last_at_most(cu, a.B, (int)i0) : 0;
-        for (int64_t i = i0; i < i0 + per && i < a.max_tokens; ++i) {
-            int64_t slot = -1;
-            int pos = 0;
-            if (i < total) {
-                while (cu[b + 1] <= i) ++b;
-                if (given_of[b] >= 0) {
-                    pos = len[b] + (int)(i - cu[b]);
-                    const int col = (int)((uint32_t)pos / (uint32_t)a.page_size), held = pages_of(len[b], a.page_size);
-                    const int page = col < held ? a.table[(int64_t)b * a.max_blocks + col]
-                                                : a.free_pages[n - 1 - (first[b] + (col - held))];
-                    if (page >= 0) slot = (int64_t)page * a.page_size + (pos - col * a.page_size);
-                }
-            }
-            a.slots[i] = slot;
-            a.positions[i] = pos;
+    for (int64_t i = id; i < a.max_tokens; i += threads) {
+        int64_t slot = -1;
+        int pos = 0;
+        const int b = i < total ? last_at_most(cu, a.B, (int)i) : -1;
+        if (b >= 0 && given_of[b] >= 0) {
+            pos = len[b] + (int)(i - cu[b]);
+            const int col = (int)((uint32_t)pos / (uint32_t)a.page_size), held = pages_of(len[b], a.page_size);
+            const int page = col < held ? a.table[(int64_t)b * a.max_blocks + col]
+                                        : a.free_pages[n - 1 - (first[b] + (col - held))];
+            if (page >= 0) slot = (int64_t)page * a.page_size + (pos - col * a.page_size);
         }
+        a.slots[i] = slot;
+        a.positions[i] = pos;
     }
 }
 
@@ -205,13 +200,32 @@ __global__ __launch_bounds__(kPageThreads) void extend_scan_kernel(ExtendArgs a)
     }
     if (ONE) {
         __syncthreads();
-        extend_fill(a, tid, blockDim.x, 1, n, given, first, lens, given_of, cu);
+        extend_fill(a, tid, blockDim.x, n, given, first, lens, given_of, cu);
     }
 }
 
+// LOCAL: the sums are brought to LDS at once (B <= kOneLaunchB); a bisection through L2 is
+// a chain of log2 B loads (64 prompts of 16 to 16384 tokens: 5.8 and 7.1 us at 4 tokens a
+// thread, 4.3 at one).
+template <bool LOCAL>
 __global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(ExtendArgs a) {
-    extend_fill(a, (int64_t)blockIdx.x * kFillThreads + threadIdx.x, (int64_t)gridDim.x * kFillThreads, kFillTokens,
-                a.st.head[0], a.st.head[1], a.st.first, a.st.len, a.st.given, a.cu);
+    const int64_t id = (int64_t)blockIdx.x * kFillThreads + threadIdx.x, threads = (int64_t)gridDim.x * kFillThreads;
+    const int n = a.st.head[0], given = a.st.head[1];
+    if constexpr (LOCAL) {
+        __shared__ int32_t local[4 * kOneLaunchB + 1];
+        for (int b = threadIdx.x; b < a.B; b += kFillThreads) {
+            local[b] = a.st.first[b];
+            local[kOneLaunchB + b] = a.st.len[b];
+            local[2 * kOneLaunchB + b] = a.st.given[b];
+            local[3 * kOneLaunchB + b] = a.cu[b];
+        }
+        if (threadIdx.x == 0) local[3 * kOneLaunchB + a.B] = a.cu[a.B];
+        __syncthreads();
+        extend_fill(a, id, threads, n, given, local, local + kOneLaunchB, local + 2 * kOneLaunchB,
+                    local + 3 * kOneLaunchB);
+    } else {
+        extend_fill(a, id, threads, n, given, a.st.first, a.st.len, a.st.given, a.cu);
+    }
 }
 
 struct ReleaseArgs {
@@ -298,7 +312,9 @@ hipError_t launch_page_extend(const PageExtend &x, hipStream_t st) {
     else hipLaunchKernelGGL((extend_scan_kernel<false, kPagePer>), dim3(1), dim3(kPageThreads), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(extend_fill_kernel, dim3(fill_grid(x.max_tokens / kFillTokens + x.B)), dim3(kFillThreads), 0, st, a);
+    const dim3 grid(fill_grid((int64_t)x.max_tokens + x.B)), block(kFillThreads);
+    if (x.B <= kOneLaunchB) hipLaunchKernelGGL(extend_fill_kernel<true>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(extend_fill_kernel<false>, grid, block, 0, st, a);
     return hipGetLastError();
 }
 
