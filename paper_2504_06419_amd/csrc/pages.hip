@@ -26,7 +26,7 @@ constexpr int kFillThreads = 256;
 
 // What the prefix sums leave for the flat pass (workspace, B entries each).
 struct PageState {
-    int32_t *head;    // [0]: free pages before, [1]: pages handed out or pushed
+    int32_t *head;    // [0]: free pages before, [1]: pages pushed (release)
     int32_t *first;   // pages of the sequences before b
     int32_t *len;     // lengths before (extend), first column pushed (release)
     int32_t *given;   // pages of b; -1: refused (extend)
@@ -110,17 +110,12 @@ __device__ __forceinline__ int last_at_most(const int32_t *v, int B, int x) {
     return lo;
 }
 
-// The flat pass, by `threads` threads of which this is `id`.  n: free pages before,
-// given: pages handed out; first, len, given_of and cu as the sums left them.
-__device__ __forceinline__ void extend_fill(const ExtendArgs &a, int64_t id, int64_t threads, int n, int given,
+// The flat pass over tokens, by `threads` threads of which this is `id`.  n: free pages
+// before; first, len, given_of and cu as the sums left them.
+__device__ __forceinline__ void extend_fill(const ExtendArgs &a, int64_t id, int64_t threads, int n,
                                             const int32_t *first, const int32_t *len, const int32_t *given_of,
                                             const int32_t *cu) {
     const int total = cu[a.B];
-    for (int64_t q = id; q < given; q += threads) {  // pages handed out
-        const int b = last_at_most(first, a.B, (int)q);
-        const int64_t col = pages_of(len[b], a.page_size) + (q - first[b]);
-        a.table[(int64_t)b * a.max_blocks + col] = a.free_pages[n - 1 - q];
-    }
     for (int64_t i = id; i < a.max_tokens; i += threads) {
         int64_t slot = -1;
         int pos = 0;
@@ -128,8 +123,9 @@ __device__ __forceinline__ void extend_fill(const ExtendArgs &a, int64_t id, int
         if (b >= 0 && given_of[b] >= 0) {
             pos = len[b] + (int)(i - cu[b]);
             const int col = (int)((uint32_t)pos / (uint32_t)a.page_size), held = pages_of(len[b], a.page_size);
-            const int page = col < held ? a.table[(int64_t)b * a.max_blocks + col]
-                                        : a.free_pages[n - 1 - (first[b] + (col - held))];
+            int32_t *const entry = a.table + (int64_t)b * a.max_blocks + col;
+            const int page = col < held ? *entry : a.free_pages[n - 1 - (first[b] + (col - held))];
+            if (col >= held && pos == col * a.page_size) *entry = page;  // the first token of a page handed out
             if (page >= 0) slot = (int64_t)page * a.page_size + (pos - col * a.page_size);
         }
         a.slots[i] = slot;
@@ -192,15 +188,12 @@ __global__ __launch_bounds__(kPageThreads) void extend_scan_kernel(ExtendArgs a)
         const int at = all_tokens > INT32_MAX ? INT32_MAX : (int)all_tokens;
         a.cu[a.B] = at;
         if (ONE) cu[a.B] = at;
-        if (!ONE) {
-            a.st.head[0] = n;
-            a.st.head[1] = given;
-        }
+        if (!ONE) a.st.head[0] = n;
         *a.n_free_out = n - given;
     }
     if (ONE) {
         __syncthreads();
-        extend_fill(a, tid, blockDim.x, n, given, first, lens, given_of, cu);
+        extend_fill(a, tid, blockDim.x, n, first, lens, given_of, cu);
     }
 }
 
@@ -210,7 +203,7 @@ __global__ __launch_bounds__(kPageThreads) void extend_scan_kernel(ExtendArgs a)
 template <bool LOCAL>
 __global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(ExtendArgs a) {
     const int64_t id = (int64_t)blockIdx.x * kFillThreads + threadIdx.x, threads = (int64_t)gridDim.x * kFillThreads;
-    const int n = a.st.head[0], given = a.st.head[1];
+    const int n = a.st.head[0];
     if constexpr (LOCAL) {
         __shared__ int32_t local[4 * kOneLaunchB + 1];
         for (int b = threadIdx.x; b < a.B; b += kFillThreads) {
@@ -221,10 +214,10 @@ __global__ __launch_bounds__(kFillThreads) void extend_fill_kernel(ExtendArgs a)
         }
         if (threadIdx.x == 0) local[3 * kOneLaunchB + a.B] = a.cu[a.B];
         __syncthreads();
-        extend_fill(a, id, threads, n, given, local, local + kOneLaunchB, local + 2 * kOneLaunchB,
+        extend_fill(a, id, threads, n, local, local + kOneLaunchB, local + 2 * kOneLaunchB,
                     local + 3 * kOneLaunchB);
     } else {
-        extend_fill(a, id, threads, n, given, a.st.first, a.st.len, a.st.given, a.cu);
+        extend_fill(a, id, threads, n, a.st.first, a.st.len, a.st.given, a.cu);
     }
 }
 
@@ -312,7 +305,7 @@ hipError_t launch_page_extend(const PageExtend &x, hipStream_t st) {
     else hipLaunchKernelGGL((extend_scan_kernel<false, kPagePer>), dim3(1), dim3(kPageThreads), 0, st, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const dim3 grid(fill_grid((int64_t)x.max_tokens + x.B)), block(kFillThreads);
+    const dim3 grid(fill_grid(x.max_tokens)), block(kFillThreads);
     if (x.B <= kOneLaunchB) hipLaunchKernelGGL(extend_fill_kernel<true>, grid, block, 0, st, a);
     else hipLaunchKernelGGL(extend_fill_kernel<false>, grid, block, 0, st, a);
     return hipGetLastError();
