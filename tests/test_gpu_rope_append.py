@@ -267,3 +267,42 @@ def test_in_a_graph_and_on_another_stream():
         call()
         torch.cuda.synchronize()
         assert all(same_bits(p, q) for p, q in zip(a, (out, kc, vc))) and kc.abs().sum() > 0
+
+
+def test_rows_behind_4_GiB():
+    """Rows whose byte offset passes 32 bits, and their neighbours."""
+    g = gen(9)
+    blocks = 60000
+    cache = torch.zeros(blocks, 64, 576, device=DEV, dtype=torch.bfloat16)  # 4.4e9 bytes
+    c, kr = randn(g, 3, 512, dt=torch.bfloat16), randn(g, 3, 64, dt=torch.bfloat16)
+    at = torch.tensor([blocks * 64 - 1, 0, 2**32 // 1152 + 1], device=DEV)
+    spire.latent_append(spire.latent_view(cache, 512), c, kr, at)
+    rows = cache.view(-1, 576)
+    assert torch.equal(rows[at], torch.cat([c, kr], 1))
+    rows[at] = 0
+    assert not any(bool(x.any()) for x in cache.split(4000))
+    blocks = 67000  # of 65536 bytes
+    kc = cache.view(-1)[:1].new_zeros(blocks, 8, 16, 256)
+    vc = torch.zeros_like(kc)
+    x = randn(g, 2, 17, 256, dt=torch.bfloat16)
+    at = torch.tensor([blocks * 16 - 1, 2**16 * 16 + 3], device=DEV)
+    table = torch.zeros(1, 1, dtype=torch.int32, device=DEV)
+    spire.qkv_append(x[:, :1], x[:, 1:9], x[:, 9:], spire.kv_view(kc, vc, table, 16), at)
+    for t, want in ((kc, x[:, 1:9]), (vc, x[:, 9:])):
+        assert torch.equal(t[at // 16, :, at % 16], want)
+        t[at // 16, :, at % 16] = 0
+        assert not any(bool(y.any()) for y in t.split(4000))
+
+
+@pytest.mark.parametrize("Dc", [512, 100])
+def test_slots_behind_32_bits(Dc):
+    """A view of more than 2^32 rows (every block the same storage)."""
+    g = gen(10)
+    cache = torch.zeros(1, 12, Dc + 64, device=DEV)
+    view = spire.latent_view(cache.expand(2**29, 12, Dc + 64), Dc)
+    c, kr = randn(g, 3, Dc), randn(g, 3, 64)
+    slots = torch.tensor([12 * (2**29 - 3) + 5, 12 * 2**29, 2**32 + 1 - (2**32 + 1) % 12 + 7], device=DEV)
+    spire.latent_append(view, c, kr, slots)
+    want = torch.zeros_like(cache)
+    want[0, 5], want[0, 7] = torch.cat([c[0], kr[0]]), torch.cat([c[2], kr[2]])
+    assert torch.equal(cache, want)
