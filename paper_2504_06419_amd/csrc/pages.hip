@@ -19,8 +19,8 @@ constexpr int kPageThreads = 1024;
 constexpr int kPagePer = 8;        // sequences a thread: B <= 8192
 constexpr int kOneLaunchB = 1024;  // sequences whose sums stand in LDS
 // Tokens up to which the flat pass is the scanning workgroup's own.  256 sequences in one
-// launch and in two, on the device: 1024 tokens 6.6 and 6.5 us, 2048 7.5 and 6.6, 4096 9.5
-// and 6.7 (1024 sequences, 1024 tokens: 7.3 and 9.5); a launch costs the host 2.5 us.
+// launch and in two, on the device: 1024 tokens 5.8 and 6.5 us, 2048 7.6 and 6.6, 4096 9.5
+// and 6.5 (1024 sequences, 1024 tokens: 7.1 and 9.5); a launch costs the host 2.5 us.
 constexpr int kOneLaunchTokens = 2048;
 constexpr int kFillThreads = 256;
 
@@ -298,7 +298,10 @@ hipError_t launch_page_extend(const PageExtend &x, hipStream_t st) {
                  page_state(x.ws, x.B)};
     if (x.B > kPageThreads * kPagePer) return hipErrorInvalidValue;
     if (x.B <= kOneLaunchB && x.max_tokens <= kOneLaunchTokens) {
-        hipLaunchKernelGGL((extend_scan_kernel<true, 1>), dim3(1), dim3(kPageThreads), 0, st, a);
+        // 512 threads start and scan sooner than 1024 (64 sequences, 320 tokens: 4.4 us against 5.9;
+        // 256 and 1024: 5.8 and 6.3), which have fewer tokens each (256 and 2048: 7.8 and 7.6)
+        const int threads = x.B <= 512 && x.max_tokens <= 1536 ? 512 : kPageThreads;
+        hipLaunchKernelGGL((extend_scan_kernel<true, 1>), dim3(1), dim3(threads), 0, st, a);
         return hipGetLastError();
     }
     if (x.B <= kPageThreads) hipLaunchKernelGGL((extend_scan_kernel<false, 1>), dim3(1), dim3(scan_threads(x.B)), 0, st, a);

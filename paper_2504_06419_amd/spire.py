@@ -431,7 +431,7 @@ def page_workspace_size(B) -> int:
 
 def _ints(*tensors):
     for t in tensors:
-        assert t.dtype == torch.int32 and t.is_contiguous()
+        assert t.dtype is torch.int32 and t.is_contiguous()
 
 
 def page_extend(block_table: torch.Tensor, page_size: int, lens: torch.Tensor, new_tokens: torch.Tensor,
