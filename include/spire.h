@@ -511,9 +511,10 @@ size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc,
  * queries have been brought into the latent's space, so every head reads the
  * same rows, as key (all Dc + Dr elements) and as value (the first Dc).
  *   q        [B, k+1, Hq, Dc + Dr] contiguous, q_dtype SPIRE_F32 or SPIRE_BF16.
- *   latent   the cache, the round's tokens appended; kv_lens [B], the mask, empty
- *            rows and lengths beyond the storage as for spire_verify_attn (k = 0:
- *            one new token a sequence).
+ *   latent   the cache, the round's tokens appended (contiguous: of at least B
+ *            sequences, num_blocks >= B); kv_lens [B], the mask, empty rows and
+ *            lengths beyond the storage as for spire_verify_attn (k = 0: one new
+ *            token a sequence).
  *   s = sm_scale * <q, row>; out [B, k+1, Hq, Dc] = sum softmax(s) latent, out_dtype
  *            SPIRE_F32 or SPIRE_BF16; lse [B, k+1, Hq] fp32 natural log, or NULL.
  *   sizes    0 <= B <= 8192, 1 <= Hq <= 128, 0 <= k <= 15, Dc 256 or 512, Dr = 64

@@ -1080,6 +1080,8 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
                               : latent->capacity <= 0 && B > 0)
         return fail(SPIRE_ERR_INVALID_ARG, "latent: a paged view needs block_table, max_blocks > 0 and num_blocks > 0, "
                                            "a contiguous one capacity > 0");
+    if (latent->page_size == 0 && B > latent->num_blocks)
+        return fail(SPIRE_ERR_INVALID_ARG, "latent: %d sequences in contiguous storage of %d (num_blocks)", B, latent->num_blocks);
     if (((uintptr_t)latent->block_table & 3u) != 0 || ((uintptr_t)latent->scale & 3u) != 0 ||
         ((uintptr_t)kv_lens & 3u) != 0 || ((uintptr_t)lse & 3u) != 0)
         return fail(SPIRE_ERR_INVALID_ARG, "block_table, scale, kv_lens and lse must be 4-byte aligned");
