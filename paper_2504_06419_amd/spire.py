@@ -528,14 +528,18 @@ def latent_view(cache: torch.Tensor, Dc: int, block_table: Optional[torch.Tensor
     capacity = size of dim 1 unless given)."""
     (blocks, tokens, Dk), (s_blk, s_tok, s_d) = cache.shape, cache.stride()
     assert s_d == 1 and 0 < Dc < Dk
-    table, rows, columns = None, 0, 0
+    assert scale is None or (scale.dtype == torch.float32 and scale.numel() >= 1)
+    table, rows, columns, sequences = None, 0, 0, blocks
     if block_table is not None:
         _ints(block_table)
-        table, rows, columns, capacity = block_table.data_ptr(), tokens, block_table.shape[1], 0
+        sequences, columns = block_table.shape
+        table, rows, capacity = block_table.data_ptr(), tokens, 0
     elif capacity is None:
         capacity = tokens
+    assert capacity <= tokens
     c = Latent(cache.data_ptr(), table, _ptr(scale), s_blk, s_tok, _DT[cache.dtype], Dc, Dk - Dc, rows, columns,
                blocks, capacity, 0)
+    c.sequences = sequences  # of this wrapper alone: what the attention may ask for
     c.keep = (cache, block_table, scale)
     return c
 
@@ -578,6 +582,9 @@ def latent_verify_attn(q: torch.Tensor, latent: Latent, kv_lens: torch.Tensor, k
     if lse is None and with_lse:
         lse = torch.empty((B, nq, Hq), dtype=torch.float32, device=q.device)
     assert out.shape == (B, nq, Hq, latent.Dc) and out.is_contiguous()
+    assert lse is None or (lse.dtype == torch.float32 and lse.numel() == B * nq * Hq and lse.is_contiguous())
+    assert kv_lens.numel() >= B and kv_lens.is_contiguous()
+    assert getattr(latent, "sequences", B) >= B, "a cache or block table of fewer sequences"
     if ws is None:
         ws = workspace(latent_workspace_size(B, Hq, k, latent.Dc, latent.Dr), q.device)
     lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)

@@ -1,0 +1,64 @@
+"""The Python calls of the serving operators refuse arrays that do not have the sizes, types and order their kernels read
+and write: the check comes before the library is called, on tensors without a GPU."""
+import pytest
+import torch
+
+from paper_2504_06419_amd import spire
+
+B, K, HQ, DC, DR = 3, 2, 4, 256, 64
+I32 = torch.int32
+
+
+@pytest.fixture
+def called(monkeypatch):
+    """Stands in for the library: counts the calls that reach it."""
+    class Lib:
+        calls = 0
+
+        def __getattr__(self, name):
+            def call(*args):
+                Lib.calls += 1
+                return 0
+            return call
+    lib = Lib()
+    monkeypatch.setattr(spire, "load", lambda *a: lib)
+    monkeypatch.setattr(spire, "_stream", lambda: 0)
+    return Lib
+
+
+def refused(called, call):
+    before = called.calls
+    with pytest.raises((AssertionError, ValueError)):
+        call()
+    assert called.calls == before
+
+
+def attention(**kw):
+    a = dict(q=torch.zeros(B, K + 1, HQ, DC + DR), cache=torch.zeros(6, 16, DC + DR), table=torch.zeros(B, 2, dtype=I32),
+             scale=None, capacity=None, lens=torch.zeros(B, dtype=I32), out=torch.zeros(B, K + 1, HQ, DC),
+             lse=torch.zeros(B, K + 1, HQ), ws=torch.zeros(256, dtype=torch.uint8))
+    a.update(kw)
+    view = spire.latent_view(a["cache"], DC, a["table"], a["scale"], a["capacity"])
+    return spire.latent_verify_attn(a["q"], view, a["lens"], K, 0.1, out=a["out"], lse=a["lse"], ws=a["ws"])
+
+
+def test_latent_attention_is_called(called):
+    attention()
+    attention(table=None)
+    attention(table=None, capacity=16)
+    attention(lens=torch.zeros(B, dtype=torch.int64))
+    attention(scale=torch.ones(1))
+    attention(lens=torch.zeros(B + 5, dtype=I32), table=torch.zeros(B + 5, 2, dtype=I32))  # of the largest batch
+    assert called.calls == 6
+
+
+@pytest.mark.parametrize("kw", [
+    dict(lens=torch.zeros(B - 1, dtype=I32)), dict(lens=torch.zeros(B - 1, dtype=torch.int64)),
+    dict(lens=torch.zeros(2 * B, dtype=I32)[::2]), dict(lens=torch.zeros(2 * B, dtype=torch.int64)[::2]),
+    dict(lse=torch.zeros(B, K + 1, HQ, dtype=torch.float64)), dict(lse=torch.zeros(B, K + 1, HQ, dtype=torch.bfloat16)),
+    dict(lse=torch.zeros(B, K, HQ)), dict(lse=torch.zeros(B, HQ, K + 1).transpose(1, 2)),
+    dict(table=torch.zeros(B - 1, 2, dtype=I32)), dict(table=torch.zeros(2 * B, dtype=I32)),
+    dict(table=torch.zeros(B, 2, dtype=torch.int64)), dict(table=None, cache=torch.zeros(B - 1, 16, DC + DR)),
+    dict(table=None, capacity=17), dict(scale=torch.ones(1, dtype=torch.float64)), dict(scale=torch.ones(0))])
+def test_latent_attention_refuses(called, kw):
+    refused(called, lambda: attention(**kw))
