@@ -447,6 +447,7 @@ def page_extend(block_table: torch.Tensor, page_size: int, lens: torch.Tensor, n
     _ints(block_table, lens, new_tokens, free_pages, n_free, positions, cu_tokens, lens_out, n_free_out)
     assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == positions.numel()
     assert lens.numel() == B and new_tokens.numel() == B and lens_out.numel() == B and cu_tokens.numel() == B + 1
+    assert n_free.numel() >= 1 and n_free_out.numel() >= 1
     if ws is None:
         ws = workspace(page_workspace_size(B), lens.device)
     _check(load().spire_page_extend(block_table.data_ptr(), page_size, max_blocks, lens.data_ptr(),
@@ -465,6 +466,7 @@ def page_release(block_table: torch.Tensor, page_size: int, lens: torch.Tensor, 
     n_free_out = n_free if n_free_out is None else n_free_out
     _ints(block_table, lens, keep, free_pages, n_free, lens_out, n_free_out)
     assert lens.numel() == B and keep.numel() == B and lens_out.numel() == B
+    assert n_free.numel() >= 1 and n_free_out.numel() >= 1
     if ws is None:
         ws = workspace(page_workspace_size(B), lens.device)
     _check(load().spire_page_release(block_table.data_ptr(), page_size, max_blocks, lens.data_ptr(),

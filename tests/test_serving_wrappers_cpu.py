@@ -62,3 +62,45 @@ def test_latent_attention_is_called(called):
     dict(table=None, capacity=17), dict(scale=torch.ones(1, dtype=torch.float64)), dict(scale=torch.ones(0))])
 def test_latent_attention_refuses(called, kw):
     refused(called, lambda: attention(**kw))
+
+
+def ints(n):
+    return torch.zeros(n, dtype=I32)
+
+
+def extend(**kw):
+    a = dict(table=torch.zeros(B, 4, dtype=I32), lens=ints(B), new=ints(B), free=ints(9), n=ints(1),
+             slots=torch.zeros(7, dtype=torch.int64), pos=ints(7), cu=ints(B + 1), lens_out=None, n_out=None)
+    a.update(kw)
+    spire.page_extend(a["table"], 16, a["lens"], a["new"], a["free"], a["n"], a["slots"], a["pos"], a["cu"],
+                      a["lens_out"], a["n_out"], torch.zeros(4096, dtype=torch.uint8))
+
+
+def release(**kw):
+    a = dict(table=torch.zeros(B, 4, dtype=I32), lens=ints(B), new=ints(B), free=ints(9), n=ints(1), lens_out=None,
+             n_out=None)
+    a.update(kw)
+    spire.page_release(a["table"], 16, a["lens"], a["new"], a["free"], a["n"], a["lens_out"], a["n_out"],
+                       torch.zeros(4096, dtype=torch.uint8))
+
+
+def test_pages_are_called(called):
+    extend()
+    extend(n_out=ints(1), lens_out=ints(B))
+    release()
+    release(n_out=ints(1), lens_out=ints(B), free=ints(0))
+    assert called.calls == 4
+
+
+@pytest.mark.parametrize("call", [extend, release])
+@pytest.mark.parametrize("kw", [
+    dict(n=ints(0)), dict(n_out=ints(0)), dict(n=torch.zeros(1, dtype=torch.int64)), dict(lens=ints(B - 1)),
+    dict(new=ints(B - 1)), dict(lens_out=ints(B - 1)), dict(free=torch.zeros(9, dtype=torch.int64)),
+    dict(lens=ints(2 * B)[::2])])
+def test_pages_refuse(called, call, kw):
+    refused(called, lambda: call(**kw))
+
+
+@pytest.mark.parametrize("kw", [dict(slots=torch.zeros(6, dtype=torch.int64)), dict(slots=ints(7)), dict(cu=ints(B))])
+def test_extend_refuses(called, kw):
+    refused(called, lambda: extend(**kw))
