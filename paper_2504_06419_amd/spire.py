@@ -199,8 +199,10 @@ def kv_view(k: torch.Tensor, v: torch.Tensor, block_table: Optional[torch.Tensor
     elif capacity is None:
         capacity = shape[2]
     # the fields in one call: one by one they are a third of a small call's time
-    return KV(k.data_ptr(), v.data_ptr(), table, _ptr(k_scale), _ptr(v_scale), stride[0], stride[1], stride[2],
-              _DT[k.dtype], rows, columns, shape[0], capacity, 0)
+    kv = KV(k.data_ptr(), v.data_ptr(), table, _ptr(k_scale), _ptr(v_scale), stride[0], stride[1], stride[2],
+            _DT[k.dtype], rows, columns, shape[0], capacity, 0)
+    kv.heads, kv.width = shape[1], shape[3]  # of this wrapper alone: spire_kv has neither, qkv_append checks them
+    return kv
 
 
 def verify_workspace_size(B, Hq, Hkv, D, k) -> int:
@@ -511,6 +513,7 @@ def qkv_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, kv: KV, slots:
     assert k.shape == (N, Hkv, D) and v.shape == k.shape and k.dtype == dtype and v.dtype == dtype
     (qs, qh, qd), (ks, kh, kd), (vs, vh, vd) = q.stride(), k.stride(), v.stride()
     assert qh == kh == vh == D and qd == kd == vd == 1, "heads must be contiguous"
+    assert getattr(kv, "heads", Hkv) >= Hkv and getattr(kv, "width", D) >= D, "a cache of fewer or shorter heads"
     assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == N
     for w in (q_weight, k_weight):
         assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == D)

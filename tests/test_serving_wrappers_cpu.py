@@ -104,3 +104,25 @@ def test_pages_refuse(called, call, kw):
 @pytest.mark.parametrize("kw", [dict(slots=torch.zeros(6, dtype=torch.int64)), dict(slots=ints(7)), dict(cu=ints(B))])
 def test_extend_refuses(called, kw):
     refused(called, lambda: extend(**kw))
+
+
+def append(cache=(4, 2, 16, 64), **kw):
+    x = torch.zeros(5, 12, 64)
+    a = dict(q=x[:, :8], k=x[:, 8:10], v=x[:, 10:], slots=torch.zeros(5, dtype=torch.int64), qw=None)
+    a.update(kw)
+    k = torch.zeros(cache)
+    view = spire.kv_view(k, torch.zeros_like(k), torch.zeros(1, 1, dtype=I32))
+    return spire.qkv_append(a["q"], a["k"], a["v"], view, a["slots"], q_weight=a["qw"])
+
+
+def test_append_is_called(called):
+    append()
+    append(cache=(4, 3, 16, 64))   # into the first heads of a cache of more
+    assert called.calls == 2
+
+
+@pytest.mark.parametrize("kw", [
+    dict(cache=(4, 1, 16, 64)), dict(cache=(4, 2, 16, 32)), dict(slots=torch.zeros(4, dtype=torch.int64)),
+    dict(slots=torch.zeros(5, dtype=I32)), dict(qw=torch.ones(32)), dict(q=torch.zeros(5, 64, 8).transpose(1, 2))])
+def test_append_refuses(called, kw):
+    refused(called, lambda: append(**kw))
