@@ -258,6 +258,13 @@ def _opts(kernel: int, opts: Optional[LaunchOpts]):
     return C.byref(opts)
 
 
+def _verify_arrays(q, kv_lens, out, lse):
+    assert kv_lens.numel() >= q.shape[0] and kv_lens.is_contiguous()
+    assert out.is_contiguous() and out.numel() == q.numel()
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and
+                           lse.numel() * q.shape[3] == q.numel())
+
+
 def verify_attn(q: torch.Tensor, kv: KV, kv_lens: torch.Tensor, Hkv: int, k: int,
                 sm_scale: float, out: Optional[torch.Tensor] = None,
                 lse: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
@@ -273,6 +280,7 @@ def verify_attn(q: torch.Tensor, kv: KV, kv_lens: torch.Tensor, Hkv: int, k: int
         lse = torch.empty((B, nq, Hq), dtype=torch.float32, device=q.device)
     if ws is None:
         ws = workspace(verify_workspace_size(B, Hq, Hkv, D, k), q.device)
+    _verify_arrays(q, kv_lens, out, lse)
     lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)
     _check(load().spire_verify_attn_ex(q.data_ptr(), _DT[q.dtype], C.byref(kv), lens.data_ptr(), B, Hq,
                                        Hkv, D, k, float(sm_scale), out.data_ptr(), _DT[out.dtype],
@@ -286,7 +294,8 @@ def verify_attn_noalloc(q: torch.Tensor, kv: KV, kv_lens: torch.Tensor, Hkv: int
     scratch instead of a workspace; the caller passes the outputs
     (out [B, k+1, Hq, D] f32 or bf16, lse [B, k+1, Hq] f32 or None)."""
     B, nq, Hq, D = q.shape
-    assert nq == k + 1 and q.is_contiguous() and out.is_contiguous()
+    assert nq == k + 1 and q.is_contiguous()
+    _verify_arrays(q, kv_lens, out, lse)
     lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)
     _check(load().spire_verify_attn_noalloc(q.data_ptr(), _DT[q.dtype], C.byref(kv), lens.data_ptr(), B, Hq,
                                             Hkv, D, k, float(sm_scale), out.data_ptr(), _DT[out.dtype],

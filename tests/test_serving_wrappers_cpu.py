@@ -126,3 +126,32 @@ def test_append_is_called(called):
     dict(slots=torch.zeros(5, dtype=I32)), dict(qw=torch.ones(32)), dict(q=torch.zeros(5, 64, 8).transpose(1, 2))])
 def test_append_refuses(called, kw):
     refused(called, lambda: append(**kw))
+
+
+def verify(noalloc=False, **kw):
+    a = dict(lens=torch.zeros(B, dtype=I32), out=torch.zeros(B, K + 1, HQ, 64), lse=torch.zeros(B, K + 1, HQ))
+    a.update(kw)
+    q, cache = torch.zeros(B, K + 1, HQ, 64), torch.zeros(B, 2, 16, 64)
+    view = spire.kv_view(cache, torch.zeros_like(cache))
+    if noalloc:
+        return spire.verify_attn_noalloc(q, view, a["lens"], 2, K, 0.1, a["out"], a["lse"])
+    return spire.verify_attn(q, view, a["lens"], 2, K, 0.1, out=a["out"], lse=a["lse"],
+                             ws=torch.zeros(256, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("noalloc", [False, True])
+def test_verify_is_called(called, noalloc):
+    verify(noalloc)
+    verify(noalloc, lens=torch.zeros(B + 2, dtype=torch.int64))
+    verify(noalloc, out=torch.zeros(B, K + 1, HQ, 64, dtype=torch.bfloat16))
+    assert called.calls == 3
+
+
+@pytest.mark.parametrize("noalloc", [False, True])
+@pytest.mark.parametrize("kw", [
+    dict(lens=torch.zeros(B - 1, dtype=I32)), dict(lens=torch.zeros(2 * B, dtype=I32)[::2]),
+    dict(lse=torch.zeros(B, K + 1, HQ, dtype=torch.float64)), dict(lse=torch.zeros(B, K, HQ)),
+    dict(lse=torch.zeros(B, HQ, K + 1).transpose(1, 2)), dict(out=torch.zeros(B, K, HQ, 64)),
+    dict(out=torch.zeros(B, K + 1, HQ, 128)[..., :64])])
+def test_verify_refuses(called, noalloc, kw):
+    refused(called, lambda: verify(noalloc, **kw))
