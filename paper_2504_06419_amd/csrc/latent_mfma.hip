@@ -44,21 +44,20 @@ typedef int s32x2 __attribute__((ext_vector_type(2)));
 // Load-to-LDS of 16 bytes per lane: lane L's bytes land at lds + 16 L.  Written as
 // assembly because the compiler orders its transposing LDS reads behind every
 // load-to-LDS that it knows of (vmcnt(0)), which would drain the ring each tile; the
-// waits are the kernel's own.  No register is written but m0, the LDS address,
-// which the compiler sets anew for each use of its own.
+// waits are the kernel's own.  No register is written but m0, the LDS address.
 template <bool NT>
 __device__ __forceinline__ void copy16_s(uint64_t base, uint32_t off, uint32_t lds) {
     if constexpr (NT)
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
     else
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(base), "s"(lds) : "memory", "m0");
 }
 template <bool NT>
 __device__ __forceinline__ void copy16_v(uint64_t addr, uint32_t lds) {
     if constexpr (NT)
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(addr), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(addr), "s"(lds) : "memory", "m0");
     else
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds) : "memory");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(addr), "s"(lds) : "memory", "m0");
 }
 
 // Workgroup barrier for LDS contents: this wave's LDS accesses are complete; copies
