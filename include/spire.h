@@ -116,7 +116,8 @@ size_t spire_verify_workspace_size(int32_t B, int32_t Hq, int32_t Hkv, int32_t D
  *   kv_lens  [B] int32: n_b; query i sees keys [0, n_b - k + i) (bottom-right
  *            causal mask).  n_b >= k+1 for a full result; smaller values are
  *            legal (rows with no visible key return zeros, lse = -inf); values
- *            above the cache capacity are clamped to it.
+ *            above the cache capacity are clamped to it, and to the smaller of
+ *            2^31 - 8192 and 16 * (floor((2^31 - 1) / B) - 1024) keys.
  *   sizes    0 <= B <= 8192, Hkv >= 1, Hq % Hkv == 0, D in {64, 128},
  *            0 <= k <= 15, (k+1) * Hq / Hkv <= 128 (SPIRE_ERR_UNSUPPORTED
  *            beyond these limits).

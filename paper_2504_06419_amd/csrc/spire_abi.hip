@@ -508,6 +508,7 @@ static spire_status verify_impl(const void *q, int32_t q_dtype, const spire_kv *
     p.kv_dtype = kv->dtype;
     p.lens = kv_lens;
     p.kv = to_dev(kv);
+    p.most_keys = most_keys(p.kv, B);
     p.out = out;
     p.out_dtype = out_dtype;
     p.lse = lse;
@@ -1106,6 +1107,7 @@ spire_status spire_latent_verify_attn_ex(const void *q, int32_t q_dtype, const s
     p.kv_dtype = latent->dtype;
     p.lens = kv_lens;
     p.kv = latent_dev(latent);
+    p.most_keys = most_keys(p.kv, B);
     p.out = out;
     p.out_dtype = out_dtype;
     p.lse = lse;

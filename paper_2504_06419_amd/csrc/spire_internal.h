@@ -64,6 +64,7 @@ struct Problem {
     int32_t q_dtype;        // SPIRE_F32 / SPIRE_BF16
     int32_t kv_dtype;
     const int32_t *lens;         // verify: kv_lens; draft: seq_lens
+    int32_t most_keys;           // verify: lengths are clamped to it
     const int32_t *ring_offset;  // draft only
     KvDev kv;               // verify cache, or the draft ring
     KvDev sink;             // draft sinks
@@ -112,16 +113,23 @@ __device__ __forceinline__ int64_t worker_of(int64_t x, int64_t T, int64_t worke
 
 constexpr int kPlanMaxB = 8192;  // sequences per call (the partition's LDS arrays)
 
-// Keys of sequence b the kernels attend to: verify lengths clamped to what
-// the cache descriptor can address, draft lengths to the sinks present plus
-// the valid ring slots.
+// The longest sequence of a verify call: what the cache descriptor can address, as far as
+// key numbers some tiles beyond the last, and the sum of all sequences' tiles (of 16 keys
+// or more) and phantoms, stay below 2^31.
+inline int32_t most_keys(const KvDev &kv, int B) {
+    const int64_t cap = kv.page_size > 0 ? (int64_t)kv.max_blocks * kv.page_size : (int64_t)kv.capacity;
+    const int64_t sum = 16 * (int64_t)(INT32_MAX / (B > 1 ? B : 1) - 1024);
+    int64_t most = INT32_MAX - 8191;
+    most = sum < most ? sum : most;
+    return (int32_t)(cap < most ? cap : most);
+}
+
+// Keys of sequence b the kernels attend to: verify lengths clamped to most_keys,
+// draft lengths to the sinks present plus the valid ring slots.
 __device__ __forceinline__ int effective_keys(const Problem &p, int b) {
     int n = p.lens[b];
     if (!p.draft) {
-        int64_t cap = p.kv.page_size > 0 ? (int64_t)p.kv.max_blocks * p.kv.page_size
-                                         : (int64_t)p.kv.capacity;
-        if (cap > INT32_MAX) cap = INT32_MAX;
-        n = n < 0 ? 0 : (n > cap ? (int)cap : n);
+        n = n < 0 ? 0 : (n > p.most_keys ? p.most_keys : n);
     } else {
         const int m = n < 0 ? 0 : n;
         const int ns = m < p.S ? m : p.S;
