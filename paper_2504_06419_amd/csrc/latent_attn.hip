@@ -166,7 +166,9 @@ __global__ __launch_bounds__(256) void latent_f32_kernel(Latent a) {
                     for (int x = 0; x < NB; ++x) {
                         const int64_t at = qrow * DC + wave * (DC / 4) + 16 * x + 4 * j;
                         uint8_t *o = static_cast<uint8_t *>(p.out) + at * (p.out_dtype == SPIRE_F32 ? 4 : 2);
-                        const float v[4] = {acc[x][0] * inv, acc[x][1] * inv, acc[x][2] * inv, acc[x][3] * inv};
+                        float v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = l == 0.f ? 0.f : acc[x][e] * inv;  // infinite values behind no weight
                         if (p.out_dtype == SPIRE_F32) store_quad<4>(o, v, 1.f);
                         else store_quad<2>(o, v, 1.f);
                     }

@@ -605,6 +605,14 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
             const float sum = alphas[16 * x + n16];
             const float inv = sum == 0.f ? 0.f : vscale / sum;
             const float lse2 = sum == 0.f ? -INFINITY : alphas[16 * NB + 16 * x + n16] * sc + log2f(sum);
+            // an empty row is zero, also where infinite values behind no weight have made its sums NaN
+            const bool empty = whole && sum == 0.f;
+            auto value = [&](int y, int x) {
+                f32x4 v = acc[y][x] * inv;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = empty ? 0.f : v[e];
+                return v;
+            };
             bool ok;
             const int64_t qrow = row_of(x, n16, ok);
             if (whole && !ok) continue;
@@ -614,13 +622,13 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
                 uint16_t *o = static_cast<uint16_t *>(A->p.out) + at;
 #pragma unroll
                 for (int y = 0; y < XB; ++y) {
-                    const f32x4 v = acc[y][x] * inv;
+                    const f32x4 v = value(y, x);
                     *reinterpret_cast<u32x2 *>(o + 16 * y) = u32x2{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
                 }
             } else {
                 float *o = (whole ? static_cast<float *>(A->p.out) : A->pl.part_o) + at;
 #pragma unroll
-                for (int y = 0; y < XB; ++y) *reinterpret_cast<f32x4 *>(o + 16 * y) = acc[y][x] * inv;
+                for (int y = 0; y < XB; ++y) *reinterpret_cast<f32x4 *>(o + 16 * y) = value(y, x);
             }
             if (wave == 0 && j == 0) {
                 if (!whole) A->pl.part_lse[row] = lse2;
