@@ -240,7 +240,9 @@ template <int DC>
 __device__ __forceinline__ void write_row(const Latent &a, int64_t qrow, int d, f32x4_t acc, float M, float L) {
     const Problem &p = a.p;
     const float inv = L == 0.f ? 0.f : 1.f / L;
-    const float v[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = L == 0.f ? 0.f : acc[e] * inv;
     if (p.out_dtype == SPIRE_F32) store_quad<4>(static_cast<uint8_t *>(p.out) + (qrow * DC + d) * 4, v, 1.f);
     else store_quad<2>(static_cast<uint8_t *>(p.out) + (qrow * DC + d) * 2, v, 1.f);
     if (d == 0 && p.lse != nullptr) p.lse[qrow] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994531f;
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(256) void latent_combine_kernel(Latent a, int per_g
             for (int x = 0; x < 4; ++x) {
                 const float w = lp[x] == -INFINITY ? 0.f : exp2f(lp[x] - ref);  // NaN: a NaN row
                 L += w;
-                if (w != 0.f) acc += w * o[x];
+                if (x0 + x < s.m) acc += w * o[x];  // 0 * NaN too: an infinite latent behind no weight
             }
         }
         write_row<DC>(a, qrow, d, acc, M, L);
@@ -340,7 +342,7 @@ __global__ __launch_bounds__(256) void latent_combine_wide_kernel(Latent a) {
             if (x0 + 16 * x < s.m) {
                 const float v = w[x0 + 16 * x], wx = v == -INFINITY ? 0.f : exp2f(v - ref);
                 L += wx;
-                if (wx != 0.f) acc += wx * o[x];
+                acc += wx * o[x];  // 0 * NaN too: an infinite latent behind no weight
             }
 #pragma unroll
         for (int x = 0; x < U; ++x)

@@ -1,5 +1,6 @@
-"""Infinite latents: the same element is part of a key and a value.  A row whose visible scores are all -inf is an empty
-row of zeros."""
+"""Infinite latents: the same element is part of a key and a value.  A key whose score is -inf weighs zero, and 0 * inf
+makes its dimension NaN in the rows that see it, however the sequence is shared out; a row whose visible scores are all
+-inf is an empty row of zeros."""
 import numpy as np
 import pytest
 import torch
@@ -44,6 +45,18 @@ def test_rows_of_nothing_but_infinite_keys(kv, kernel, Hq, k, Dc, ps):
             r[0] = -float("inf")
     o, l = compare(inp, kernel)
     assert np.isneginf(l[:2]).all() and (o[:2] == 0).all() and np.isfinite(o[2:, k]).all()
+
+
+@FORMS
+@pytest.mark.parametrize("lens", [[6000], [70, 200] * 150, [4000] * 40, [3000, 5] * 30])
+def test_infinite_keys_among_others(kv, kernel, lens):
+    """One workgroup a sequence, a few, many: the first 64 keys (whole tiles, and whole shares of long sequences)."""
+    inp = inputs(lens, kv, 16, 0, 256, 64)
+    for b in range(0, len(lens), 2):
+        for r in rows(inp, b, range(min(64, lens[b] - 1))):
+            r[0] = -float("inf")
+    o, l = compare(inp, kernel)
+    assert np.isnan(o[::2, 0, :, 0]).all() and np.isfinite(o[::2, 0, :, 1:]).all() and np.isfinite(l).all()
 
 
 @FORMS
