@@ -522,9 +522,11 @@ size_t spire_latent_workspace_size(int32_t B, int32_t Hq, int32_t k, int32_t Dc,
  *            (SPIRE_ERR_UNSUPPORTED otherwise).
  *   workspace >= spire_latent_workspace_size(B, Hq, k, Dc, Dr) bytes, 256-byte aligned.
  * bf16 queries on bf16 or fp8 caches whose rows start 16-byte aligned run on the
- * 16-bit matrix instructions (probabilities rounded to 16 bits, sums in fp32),
- * everything else in fp32.  Non-finite values act as for spire_verify_attn;
- * a key that a row does not see never influences it, whatever it holds.
+ * 16-bit matrix instructions (probabilities rounded to bf16 for bf16 caches; for
+ * fp8 caches to fp16, those below 2^-21 of the largest of a row to multiples of
+ * about 2^-31 of it; sums in fp32), everything else in fp32.  Non-finite and very
+ * large values act as for spire_verify_attn; a key that a row does not see never
+ * influences it, whatever it holds.
  */
 spire_status spire_latent_verify_attn(const void *q, int32_t q_dtype, const spire_latent *latent,
                                       const int32_t *kv_lens, int32_t B, int32_t Hq, int32_t k,

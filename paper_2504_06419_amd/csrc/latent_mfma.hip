@@ -93,6 +93,15 @@ template <class V> __device__ __forceinline__ V lds_read(uint32_t at) {
 template <bool FP8> __device__ __forceinline__ bool not_finite(uint32_t at) {
     return FP8 ? (lds_read<uint8_t>(at) & 0x7F) == 0x7F : (lds_read<uint16_t>(at) & 0x7F80) == 0x7F80;
 }
+// Probabilities are rounded to the values' operand type, as one matrix instruction takes
+// both (bf16 rows: bf16, 8 bits; fp8 rows: fp16, 11 bits), their sum is not: the row sum
+// and the log-sum-exp keep fp32. A second product for the rest of a probability would cost
+// another matrix pass. fp16 holds a narrow range, so fp8 rows' probabilities are lifted to
+// its upper end: 2^8 above the reference, the most that a lazy reference leaves, is 2^15,
+// and what is lost begins at 2^-32 of the reference instead of 2^-25 (4096 keys of 2^-26
+// behind a first key of 1 came out as 0).
+template <bool FP8> constexpr float kLift = FP8 ? 7.f : 0.f;
+
 // Registers that loads fill: has the compiler wait for them here.  Without it the
 // wait stands at their first use in the tile loop and, taken every time round,
 // also waits for the copies in flight.
@@ -454,7 +463,7 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
                     for (int y = 0; y < KT; ++y) {
                         float e[4];
 #pragma unroll
-                        for (int z = 0; z < 4; ++z) e[z] = fast_exp2((s[0][y][z] - msub) * sc);
+                        for (int z = 0; z < 4; ++z) e[z] = fast_exp2(fmaf(s[0][y][z] - msub, sc, kLift<FP8>));
                         l += (e[0] + e[1]) + (e[2] + e[3]);
                         const u32x2 v = {pack_p<FP8>(e[0], e[1]), pack_p<FP8>(e[2], e[3])};
                         *reinterpret_cast<__attribute__((address_space(3))) u32x2 *>((lds_u8 *)(uintptr_t)((pwrite0 ^ (32 * y)) + buf * PB)) = v;
@@ -604,7 +613,7 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
         for (int x = 0; x < NB; ++x) {
             const float sum = alphas[16 * x + n16];
             const float inv = sum == 0.f ? 0.f : vscale / sum;
-            const float lse2 = sum == 0.f ? -INFINITY : alphas[16 * NB + 16 * x + n16] * sc + log2f(sum);
+            const float lse2 = sum == 0.f ? -INFINITY : alphas[16 * NB + 16 * x + n16] * sc + (log2f(sum) - kLift<FP8>);
             // an empty row is zero, also where infinite values behind no weight have made its sums NaN
             const bool empty = whole && sum == 0.f;
             auto value = [&](int y, int x) {
