@@ -53,7 +53,7 @@ __device__ __forceinline__ bool latent_start(const Latent &a, int g, int u, int3
     return some;
 }
 
-// Positions of sequence b: its tiles and the phantoms of its segment.
+// Tiles of a sequence of n keys: without keys one, empty, so that its rows are written.
 template <int TILE>
 __device__ __forceinline__ int latent_tiles(int n) { return n > 0 ? (n + TILE - 1) / TILE : 1; }
 

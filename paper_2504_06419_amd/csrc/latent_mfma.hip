@@ -19,10 +19,11 @@
 // not (8 units of 64 rows that share their keys in L2: 2.4 us a tile of 64 keys
 // without any arithmetic), so rows that share keys belong into one workgroup: 128
 // rows are what its registers hold (128 accumulators and 72 queries of 256).
-// A K operand read from LDS serves two row blocks, so LDS delivers 272 16-byte reads
-// (2176 cycles) for the 272 matrix instructions a SIMD issues (2176) on a 32-key tile
-// of 512 dimensions and 128 rows; with a wave per block and all dimensions it is 384
-// (measured without copies: 2.4 us a tile).
+// A K operand read from LDS serves two row blocks: on a 32-key tile of 512 dimensions
+// and 128 rows the workgroup makes 272 LDS accesses of 16 bytes a lane (144 of K, 32 of
+// C, 64 of P, 32 of swapped halves; 8 cycles each, 2176) while a SIMD's two waves issue
+// 136 matrix instructions (36 and 32 a wave; 16 cycles each, 2176).  With a wave per
+// block and all dimensions it is 384 accesses (measured without copies: 2.4 us a tile).
 //
 // What bounds it: HBM up to 64 bf16 rows (64 sequences of 16384: 16 rows 6.3 TB/s, 64
 // rows 5.7); at 128 rows the products and what stands between them, barriers,
@@ -144,7 +145,9 @@ __global__ __launch_bounds__(512, 2) void latent_mfma_kernel(Latent a) {
     // Waves without rows to score copy the tiles; with 7 and 8 blocks every wave does its share.
     constexpr int CW = NB <= 4 ? 4 : (NB <= 6 ? 2 : 8), TILE = latent_tile(true, DC * (FP8 ? 1 : 2), NB), SCAN = TILE / 8;  // copying waves; rows a wave looks through
     using G = LatStage<DC, FP8, CW, TILE>;
-    constexpr bool NT = NB <= 4;  // up to 4 blocks are one unit: its rows are read once, and streamed
+    // Streaming copies for up to 4 blocks: those are always a sequence's only unit, so its rows
+    // are read once.  5 to 8 blocks can be one unit of several that share them through L2.
+    constexpr bool NT = NB <= 4;
     constexpr int DK = DC + kLatentDr, KT = G::KT;
     constexpr int STEPS = DK / 32;      // QK steps of 32 dimensions
     constexpr int XB = DC / 128;        // 16-dimension output blocks of a wave
