@@ -258,11 +258,15 @@ def _opts(kernel: int, opts: Optional[LaunchOpts]):
     return C.byref(opts)
 
 
-def _verify_arrays(q, kv_lens, out, lse):
-    assert kv_lens.numel() >= q.shape[0] and kv_lens.is_contiguous()
-    assert out.is_contiguous() and out.numel() == q.numel()
-    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and
-                           lse.numel() * q.shape[3] == q.numel())
+# A call's own outputs are right as allocated: what is checked costs host time (0.1 us an attribute).
+def _verify_outputs(out, lse, rows, D):
+    assert out is None or (out.numel() == rows * D and out.is_contiguous())
+    assert lse is None or (lse.dtype is torch.float32 and lse.numel() == rows and lse.is_contiguous())
+
+
+def _verify_lens(lens, B):
+    assert lens.numel() >= B and lens.is_contiguous()
+    return lens if lens.dtype is torch.int32 else lens.to(torch.int32)
 
 
 def verify_attn(q: torch.Tensor, kv: KV, kv_lens: torch.Tensor, Hkv: int, k: int,
@@ -274,14 +278,14 @@ def verify_attn(q: torch.Tensor, kv: KV, kv_lens: torch.Tensor, Hkv: int, k: int
     events).  q [B, k+1, Hq, D]; returns (out, lse)."""
     B, nq, Hq, D = q.shape
     assert nq == k + 1 and q.is_contiguous()
+    _verify_outputs(out, lse, B * nq * Hq, D)
     if out is None:
         out = torch.empty((B, nq, Hq, D), dtype=out_dtype, device=q.device)
     if lse is None and with_lse:
         lse = torch.empty((B, nq, Hq), dtype=torch.float32, device=q.device)
     if ws is None:
         ws = workspace(verify_workspace_size(B, Hq, Hkv, D, k), q.device)
-    _verify_arrays(q, kv_lens, out, lse)
-    lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)
+    lens = _verify_lens(kv_lens, B)
     _check(load().spire_verify_attn_ex(q.data_ptr(), _DT[q.dtype], C.byref(kv), lens.data_ptr(), B, Hq,
                                        Hkv, D, k, float(sm_scale), out.data_ptr(), _DT[out.dtype],
                                        _ptr(lse), ws.data_ptr(), ws.numel(), _stream(), _opts(kernel, opts)))
@@ -295,8 +299,8 @@ def verify_attn_noalloc(q: torch.Tensor, kv: KV, kv_lens: torch.Tensor, Hkv: int
     (out [B, k+1, Hq, D] f32 or bf16, lse [B, k+1, Hq] f32 or None)."""
     B, nq, Hq, D = q.shape
     assert nq == k + 1 and q.is_contiguous()
-    _verify_arrays(q, kv_lens, out, lse)
-    lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)
+    _verify_outputs(out, lse, B * nq * Hq, D)
+    lens = _verify_lens(kv_lens, B)
     _check(load().spire_verify_attn_noalloc(q.data_ptr(), _DT[q.dtype], C.byref(kv), lens.data_ptr(), B, Hq,
                                             Hkv, D, k, float(sm_scale), out.data_ptr(), _DT[out.dtype],
                                             _ptr(lse), _stream()))
@@ -589,19 +593,18 @@ def latent_verify_attn(q: torch.Tensor, latent: Latent, kv_lens: torch.Tensor, k
                        kernel: int = 0, opts: Optional[LaunchOpts] = None):
     """spire_latent_verify_attn (the _ex form with a kernel choice or launch events).
     q [B, k+1, Hq, Dc + Dr]; returns (out [B, k+1, Hq, Dc], lse [B, k+1, Hq])."""
-    B, nq, Hq, Dk = q.shape
-    assert nq == k + 1 and q.is_contiguous() and Dk == latent.Dc + latent.Dr
+    (B, nq, Hq, Dk), Dc = q.shape, latent.Dc
+    assert nq == k + 1 and q.is_contiguous() and Dk == Dc + latent.Dr
+    assert out is None or out.shape == (B, nq, Hq, Dc)
+    _verify_outputs(out, lse, B * nq * Hq, Dc)
     if out is None:
-        out = torch.empty((B, nq, Hq, latent.Dc), dtype=out_dtype, device=q.device)
+        out = torch.empty((B, nq, Hq, Dc), dtype=out_dtype, device=q.device)
     if lse is None and with_lse:
         lse = torch.empty((B, nq, Hq), dtype=torch.float32, device=q.device)
-    assert out.shape == (B, nq, Hq, latent.Dc) and out.is_contiguous()
-    assert lse is None or (lse.dtype == torch.float32 and lse.numel() == B * nq * Hq and lse.is_contiguous())
-    assert kv_lens.numel() >= B and kv_lens.is_contiguous()
     assert getattr(latent, "sequences", B) >= B, "a cache or block table of fewer sequences"
     if ws is None:
-        ws = workspace(latent_workspace_size(B, Hq, k, latent.Dc, latent.Dr), q.device)
-    lens = kv_lens if kv_lens.dtype == torch.int32 else kv_lens.to(torch.int32)
+        ws = workspace(latent_workspace_size(B, Hq, k, Dc, latent.Dr), q.device)
+    lens = _verify_lens(kv_lens, B)
     _check(load().spire_latent_verify_attn_ex(q.data_ptr(), _DT[q.dtype], C.byref(latent), lens.data_ptr(), B, Hq, k,
                                               float(sm_scale), out.data_ptr(), _DT[out.dtype], _ptr(lse),
                                               ws.data_ptr(), ws.numel(), _stream(), _opts(kernel, opts)))
