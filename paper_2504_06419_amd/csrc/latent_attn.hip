@@ -7,10 +7,12 @@
 // its quarter of the Dc + 64 dimensions (v_mfma_f32_16x16x4_f32, S^T = K Q^T); the
 // quarters meet in LDS and every wave takes the online softmax of all 32 keys;
 // then wave w accumulates its quarter of the latent, O^T += C^T P^T.  The path of
-// full precision checks: its calls are short chains of dependent steps (4 sequences
-// of 512 rows of 320, 8 heads, k = 4: 17.5 us and 8 for the merge), and of long ones
-// fp32 products and conversions on the way into LDS set the time (64 sequences of 512
-// to 16384 bf16 rows, 16 heads, k = 4: 2.8 ms).
+// full precision checks.  Nothing is in flight while a tile is scored, and each 16-row
+// block is a workgroup of its own that reads and converts every row again, so a small
+// call is a chain of dependent steps (4 sequences of 512 rows of 320, 8 heads, k = 4:
+// 16.7 us and 5.2 for the merge) and a large one waits at every tile (64 sequences of
+// 512 to 16384 rows, 16 heads, k = 4: 2.8 ms bf16, 3.0 ms fp32; its products are about
+// 0.33 ms at the peak of the fp32 matrix instructions).
 #include "convert.h"
 #include "combine.h"
 #include "latent_common.h"
@@ -193,7 +195,7 @@ __global__ __launch_bounds__(256) void latent_f32_kernel(Latent a) {
 // out = sum_i w_i o_i / sum_i w_i with w_i = 2^(lse_i - max).  A workgroup takes one
 // sequence (or, with more sequences than groups, the one that group g is the first
 // to start inside of).  What bounds it is the partials, written and read once: 100
-// MB for 128 sequences of 128 rows of 512 on 256 groups (30 us, 3.4 TB/s).
+// MB for 128 sequences of 128 rows of 512 on 256 groups (26 us, 3.8 TB/s).
 struct Split {
     int b, m;            // sequence, partials; m = 0: nothing to merge
     int64_t start, wlo, T, workers;

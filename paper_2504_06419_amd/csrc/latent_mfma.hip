@@ -25,12 +25,14 @@
 // 136 matrix instructions (36 and 32 a wave; 16 cycles each, 2176).  With a wave per
 // block and all dimensions it is 384 accesses (measured without copies: 2.4 us a tile).
 //
-// What bounds it: HBM up to 64 bf16 rows (64 sequences of 16384: 16 rows 6.3 TB/s, 64
-// rows 5.7); at 128 rows the products and what stands between them, barriers,
+// What bounds it: HBM up to 64 bf16 rows (64 sequences of 16384: 16 rows 6.5 TB/s, 64
+// rows 5.5); at 128 rows the products and what stands between them, barriers,
 // exponentials and exchanges, which two waves a SIMD overlap in part (128 heads, k =
-// 3: 800 TFLOP/s of the 1135 of a large library product); with 16 fp8 rows the
-// barriers of a tile (4.5 TB/s: without copies 154 of 176 us, without scores 136,
-// without probabilities 157 on tiles of 32 keys).
+// 3: 915 TFLOP/s of the 1135 of a large library product); with 16 fp8 rows the
+// barriers of a tile (5.0 TB/s: without copies 154 of 176 us, without scores 136,
+// without probabilities 157 on tiles of 32 keys); with few tiles a workgroup the start
+// of a segment, which waits for the whole ring before its first scores.  An odd number
+// of blocks leaves the last pair of waves one that is not there, scored all the same.
 #include <type_traits>
 
 #include "latent_common.h"
