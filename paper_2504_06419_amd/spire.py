@@ -265,8 +265,9 @@ def _verify_outputs(out, lse, rows, D):
 
 
 def _verify_lens(lens, B):
+    lens = lens if lens.dtype is torch.int32 else lens.to(torch.int32)  # a copy is contiguous
     assert lens.numel() >= B and lens.is_contiguous()
-    return lens if lens.dtype is torch.int32 else lens.to(torch.int32)
+    return lens
 
 
 def verify_attn(q: torch.Tensor, kv: KV, kv_lens: torch.Tensor, Hkv: int, k: int,

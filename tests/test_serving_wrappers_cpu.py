@@ -47,14 +47,15 @@ def test_latent_attention_is_called(called):
     attention(table=None)
     attention(table=None, capacity=16)
     attention(lens=torch.zeros(B, dtype=torch.int64))
+    attention(lens=torch.zeros(2 * B, dtype=torch.int64)[::2])  # converted, and so in order
     attention(scale=torch.ones(1))
     attention(lens=torch.zeros(B + 5, dtype=I32), table=torch.zeros(B + 5, 2, dtype=I32))  # of the largest batch
-    assert called.calls == 6
+    assert called.calls == 7
 
 
 @pytest.mark.parametrize("kw", [
     dict(lens=torch.zeros(B - 1, dtype=I32)), dict(lens=torch.zeros(B - 1, dtype=torch.int64)),
-    dict(lens=torch.zeros(2 * B, dtype=I32)[::2]), dict(lens=torch.zeros(2 * B, dtype=torch.int64)[::2]),
+    dict(lens=torch.zeros(2 * B, dtype=I32)[::2]),
     dict(lse=torch.zeros(B, K + 1, HQ, dtype=torch.float64)), dict(lse=torch.zeros(B, K + 1, HQ, dtype=torch.bfloat16)),
     dict(lse=torch.zeros(B, K, HQ)), dict(lse=torch.zeros(B, HQ, K + 1).transpose(1, 2)),
     dict(table=torch.zeros(B - 1, 2, dtype=I32)), dict(table=torch.zeros(2 * B, dtype=I32)),
@@ -143,8 +144,9 @@ def verify(noalloc=False, **kw):
 def test_verify_is_called(called, noalloc):
     verify(noalloc)
     verify(noalloc, lens=torch.zeros(B + 2, dtype=torch.int64))
+    verify(noalloc, lens=torch.zeros(2 * B, dtype=torch.int64)[::2])
     verify(noalloc, out=torch.zeros(B, K + 1, HQ, 64, dtype=torch.bfloat16))
-    assert called.calls == 3
+    assert called.calls == 4
 
 
 @pytest.mark.parametrize("noalloc", [False, True])
